@@ -1,0 +1,536 @@
+"""What is measured of the network operators (normalisation, causal convolution,
+selective scan, orthogonalised updates): the cases, their inputs, one pass of
+each in plain torch operations and through the library, and the same outputs
+in 64 bits.
+
+The operators are those of a time-marching network whose output fields the
+residual operators judge.  A "sequence" is the time levels at one grid node (or
+a grid's nodes in scan order), a "channel" one feature of the network there.
+With ``own`` false ``run`` computes everything in elementary torch operations
+in 32 bits; with ``own`` true it makes the library's calls.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+EPS = 1e-6                              # the norm's
+NS_COEFFS = (3.4445, -4.7750, 2.0315)   # the quintic's a, b, c
+NS_STEPS, NS_EPS = 5, 1e-7
+MUON = {"lr": 0.02, "momentum": 0.95, "weight_decay": 0.01}
+F8_MAX = 448.0                          # largest finite e4m3 value
+F8_TINY = 2.0 ** -126                   # smallest scale of a group
+
+
+def listed():
+    return [
+        # one time level of 64 nodes of a rollout enters a block in 8 bits
+        dict(name="norm f8, 64 x 256", kind="norm8", rows=64, width=256, type="bf16", group=128),
+        # a surrogate's activations over part of a grid, odd row count, ragged last group
+        dict(name="norm f8, 50021 x 1160", kind="norm8", rows=50021, width=1160, type="bf16", group=128),
+        # training on the Burgers grid (128 x 256 nodes), the widest network of the paper
+        dict(name="norm train, 32768 x 256", kind="norm", rows=32768, width=256, type="f32"),
+        # training on the Helmholtz grid (1024 x 1024 nodes)
+        dict(name="norm train, 1048576 x 128", kind="norm", rows=1048576, width=128, type="bf16"),
+        # the Burgers grid as 256 sequences of 128 time levels, twice the widest network's channels
+        dict(name="conv train, 256 x 128 x 512", kind="conv", train=True, batch=256, length=128, channels=512,
+             taps=4, type="bf16"),
+        # a prompt of odd lengths, three taps
+        dict(name="conv prompt, 3 x 1021 x 200", kind="conv", train=False, batch=3, length=1021, channels=200,
+             taps=3, type="f32"),
+        # a long prompt: a 128 x 128 grid's nodes in scan order, few sequences
+        dict(name="scan prompt, 2 x 16384 x 512", kind="scan", train=False, batch=2, length=16384, channels=512,
+             states=16, groups=1, type="f32"),
+        # training on long windows
+        dict(name="scan train, 8 x 2048 x 1024", kind="scan", train=True, batch=8, length=2048, channels=1024,
+             states=16, groups=1, type="bf16"),
+        # one time level of a rollout at 256 nodes: convolution and scan with their carried states
+        dict(name="step, 256 x 512", kind="step", batch=256, channels=512, states=16, groups=1, taps=4, type="bf16"),
+        # the update of a network of the paper's width 128
+        dict(name="muon, 6 of 128 x 128", kind="muon", count=6, m=128, n=128, type="f32"),
+        # in and out projections of a small block, not square
+        dict(name="orthogonalize, 4 of 260 x 1000", kind="ortho", count=4, m=260, n=1000, type="f32"),
+        # one large matrix in 16 bits
+        dict(name="muon, 4096 x 4096", kind="muon", count=1, m=4096, n=4096, type="bf16"),
+    ]
+
+
+def _log(rng, lo, hi):
+    """A whole number in [lo, hi], spread over its logarithm."""
+    return min(hi, max(lo, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def _some(rng, lo, hi, step):
+    """As _log, a multiple of `step` two times in three."""
+    v = _log(rng, lo, hi)
+    return v if rng.random() < 1 / 3 else min(hi, max(lo, (v + step // 2) // step * step or step))
+
+
+def draw(rng):
+    kind = rng.choice(("norm8", "norm", "conv", "scan", "step", "muon", "ortho"))
+    typ = rng.choice(("f32", "bf16", "f16"))
+    if kind in ("norm8", "norm"):
+        width = _some(rng, 16, 8192, 64)
+        rows = _log(rng, 1, min(1 << 20, (1 << 26) // width))
+        case = dict(kind=kind, rows=rows, width=width, type=typ)
+        if kind == "norm8":
+            case["group"] = rng.choice((128, 128, 0))
+        return case
+    if kind in ("conv", "scan"):
+        train = rng.random() < 0.5
+        length = _log(rng, 1, 16384)
+        channels = _some(rng, 8, 2048, 64)
+        most = 1 << (23 if kind == "scan" else 24)
+        batch = _log(rng, 1, max(1, min(256, most // (length * channels))))
+        length = min(length, max(1, most // (batch * channels)))
+        case = dict(kind=kind, train=train, batch=batch, length=length, channels=channels, type=typ)
+        if kind == "conv":
+            case["taps"] = rng.choice((2, 3, 4))
+        else:
+            case["states"] = rng.choice((4, 8, 16, 16, 16, 24, 32))
+            case["groups"] = rng.choice((1, 1, 2)) if channels % 2 == 0 else 1
+        return case
+    if kind == "step":
+        channels = _some(rng, 32, 4096, 64)
+        return dict(kind=kind, batch=_log(rng, 1, min(4096, (1 << 20) // channels)), channels=channels,
+                    states=rng.choice((4, 8, 16, 16, 16, 32)), groups=1, taps=rng.choice((2, 3, 4)), type=typ)
+    m, n = _some(rng, 16, 2048, 32), _some(rng, 16, 2048, 32)
+    count = max(1, min(_log(rng, 1, 12), (1 << 22) // (m * n)))
+    return dict(kind=kind, count=count, m=m, n=n, type=typ)
+
+
+# ---------------------------------------------------------------------------
+# Inputs.
+
+def _randn(g, *shape):
+    return torch.randn(*shape, generator=g, device="cuda", dtype=torch.float32)
+
+
+def _rand(g, *shape):
+    return torch.rand(*shape, generator=g, device="cuda", dtype=torch.float32)
+
+
+def _lengths(g, batch, length):
+    """Ragged windows: every sequence holds between half and all of its levels, the first all."""
+    lo = length - length // 2
+    v = torch.randint(lo, length + 1, (batch,), generator=g, device="cuda", dtype=torch.int32)
+    v[0] = length
+    return v
+
+
+def _scan_params(g, channels, states):
+    """Decay rates 1..N and step sizes between 0.001 and 0.1, as such networks start from."""
+    A = -torch.arange(1, states + 1, device="cuda", dtype=torch.float32).expand(channels, states)
+    A = (A * (1 + 0.1 * _randn(g, channels, states).clamp(-3, 3))).contiguous()
+    dt = torch.exp(_rand(g, channels) * math.log(100.0) + math.log(1e-3))
+    return dict(A=A, bias=dt + torch.log(-torch.expm1(-dt)), D=1 + 0.1 * _randn(g, channels))
+
+
+def prepare(case, seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    T = TYPES[case["type"]]
+    k = case["kind"]
+    s = dict(case=case)
+    if k in ("norm8", "norm"):
+        rows, width = case["rows"], case["width"]
+        s["x"] = _randn(g, rows, width).to(T)
+        s["r"] = (2 * _randn(g, rows, width)).to(T)
+        s["w"] = 1 + 0.2 * _randn(g, width)
+        if k == "norm":
+            s["dy"] = _randn(g, rows, width).to(T)
+            s["ds"] = _randn(g, rows, width).to(T)
+    elif k == "conv":
+        B, L, D, W = case["batch"], case["length"], case["channels"], case["taps"]
+        s["x"] = _randn(g, B, L, D).to(T)
+        s["w"] = _randn(g, D, W) / math.sqrt(W)
+        s["b"] = 0.1 * _randn(g, D)
+        s["lengths"] = _lengths(g, B, L)
+        if case["train"]:
+            s["dy"] = _randn(g, B, L, D).to(T)
+    elif k == "scan":
+        B, L, D, N, G = (case[n] for n in ("batch", "length", "channels", "states", "groups"))
+        s["u"] = _randn(g, B, L, D).to(T)
+        s["delta"] = (0.5 * _randn(g, B, L, D)).to(T)
+        s["B"] = _randn(g, B, L, G, N).to(T)
+        s["C"] = _randn(g, B, L, G, N).to(T)
+        s["z"] = _randn(g, B, L, D).to(T)
+        s["lengths"] = _lengths(g, B, L)
+        s.update(_scan_params(g, D, N))
+        if case["train"]:
+            s["dy"] = _randn(g, B, L, D).to(T)
+    elif k == "step":
+        B, D, N, G, W = (case[n] for n in ("batch", "channels", "states", "groups", "taps"))
+        s["x"] = _randn(g, B, D).to(T)
+        s["conv_state"] = _randn(g, B, W - 1, D).to(T)
+        s["w"] = _randn(g, D, W) / math.sqrt(W)
+        s["b"] = 0.1 * _randn(g, D)
+        s["state"] = _randn(g, B, D, N)
+        s["delta"] = (0.5 * _randn(g, B, D)).to(T)
+        s["B"] = _randn(g, B, G, N).to(T)
+        s["C"] = _randn(g, B, G, N).to(T)
+        s["z"] = _randn(g, B, D).to(T)
+        s.update(_scan_params(g, D, N))
+    else:
+        # gradients with a decaying spectrum beside noise
+        c, m, n = case["count"], case["m"], case["n"]
+        q = max(1, min(m, n) // 8)
+        low = torch.matmul(_randn(g, c, m, q), _randn(g, c, q, n)) / math.sqrt(q)
+        s["G"] = (1e-3 * (low + 0.5 * _randn(g, c, m, n))).to(T)
+        if k == "muon":
+            s["M"] = 1e-2 * _randn(g, c, m, n)
+            s["Wt"] = (_randn(g, c, m, n) / math.sqrt(n)).to(T)
+    return s
+
+
+# ---------------------------------------------------------------------------
+# One pass.
+
+def run(state):
+    return (_run_own if own else _run_plain)(state)
+
+
+def _run_own(s):
+    from paper_2607_18020_amd import network as N
+    case = s["case"]
+    k = case["kind"]
+    if k == "norm8":
+        q, scales, total = N.fpde_rms_norm(s["x"], s["w"], residual=s["r"], eps=EPS, quant=case["group"])
+        return dict(q=q, scales=scales, s=total)
+    if k == "norm":
+        y, total = N.fpde_rms_norm(s["x"], s["w"], residual=s["r"], eps=EPS)
+        dx, dw = N.fpde_rms_norm_bwd(s["dy"], total, s["w"], dsum=s["ds"], eps=EPS)
+        return dict(y=y, s=total, dx=dx, dw=dw)
+    if k == "conv":
+        D, W = s["w"].shape
+        if not case["train"]:
+            last = torch.empty(case["batch"], W - 1, D, dtype=s["x"].dtype, device="cuda")
+            y = N.fpde_causal_conv(s["x"], s["w"], s["b"], lengths=s["lengths"], state_out=last)
+            return dict(y=y, state=last)
+        y = N.fpde_causal_conv(s["x"], s["w"], s["b"], lengths=s["lengths"])
+        dx, dw, db = N.fpde_causal_conv_bwd(s["dy"], s["x"], s["w"], s["b"], lengths=s["lengths"])
+        return dict(y=y, dx=dx, dw=dw, db=db)
+    if k == "scan":
+        args = (s["u"], s["delta"], s["A"], s["B"], s["C"])
+        opts = dict(D=s["D"], z=s["z"], delta_bias=s["bias"], softplus=True, lengths=s["lengths"])
+        if not case["train"]:
+            last = torch.empty(case["batch"], *s["A"].shape, dtype=torch.float32, device="cuda")
+            y = N.fpde_selective_scan(*args, state_out=last, **opts)
+            return dict(y=y, state=last)
+        y = N.fpde_selective_scan(*args, **opts)
+        g = N.fpde_selective_scan_bwd(s["dy"], *args, **opts)
+        return dict(y=y, du=g.du, ddelta=g.ddelta, dA=g.dA, dB=g.dB, dC=g.dC, dD=g.dD, dz=g.dz, dbias=g.ddelta_bias)
+    if k == "step":
+        c = N.fpde_causal_conv_step(s["x"], s["conv_state"], s["w"], s["b"])
+        y = N.fpde_selective_step(s["state"], c, s["delta"], s["A"], s["B"], s["C"], D=s["D"], z=s["z"],
+                                  delta_bias=s["bias"], softplus=True)
+        return dict(c=c, conv_state=s["conv_state"], y=y, state=s["state"])
+    if k == "ortho":
+        return dict(o=N.fpde_orthogonalize(s["G"], steps=NS_STEPS, coeffs=NS_COEFFS, eps=NS_EPS))
+    N.fpde_muon_step(s["Wt"].unbind(0), s["G"].unbind(0), s["M"].unbind(0), nesterov=True, steps=NS_STEPS,
+                     coeffs=NS_COEFFS, eps=NS_EPS, **MUON)
+    return dict(w=s["Wt"], m=s["M"])
+
+
+def _silu(x):
+    return x / (1 + torch.exp(-x))
+
+
+def _dsilu(x):
+    q = 1 / (1 + torch.exp(-x))
+    return q * (1 + x * (1 - q))
+
+
+def _softplus(x):
+    return torch.clamp(x, min=0) + torch.log1p(torch.exp(-torch.abs(x)))
+
+
+def _valid(s, L):
+    return (torch.arange(L, device="cuda")[None, :] < s["lengths"][:, None])[..., None]
+
+
+def _linear_scan(a, b):
+    """h_t = a_t h_{t-1} + b_t along dim 1 from h = 0, by doubling: log2(L) rounds over the whole window."""
+    off = 1
+    while off < a.shape[1]:
+        b = torch.cat((b[:, :off], torch.addcmul(b[:, off:], a[:, off:], b[:, :-off])), 1)
+        a = torch.cat((a[:, :off], a[:, off:] * a[:, :-off]), 1)
+        off *= 2
+    return b
+
+
+def _per_channel(v, D):
+    """[..., G, N] -> [..., D, N]: the group of each channel."""
+    return v.repeat_interleave(D // v.shape[-2], dim=-2)
+
+
+def _run_plain(s):
+    case = s["case"]
+    k = case["kind"]
+    T = TYPES[case["type"]]
+    if k in ("norm8", "norm"):
+        t = s["x"].float() + s["r"].float()
+        y = t * torch.rsqrt((t * t).mean(-1, keepdim=True) + EPS) * s["w"]
+        total = t.to(T)
+        if k == "norm8":
+            rows, width = y.shape
+            g = case["group"] or width
+            ng = -(-width // g)
+            yg = torch.nn.functional.pad(y, (0, ng * g - width)).view(rows, ng, g)
+            scales = torch.clamp(yg.abs().amax(-1) / F8_MAX, min=F8_TINY)
+            q = torch.clamp(yg / scales[..., None], -F8_MAX, F8_MAX).view(rows, ng * g)[:, :width]
+            return dict(q=q.to(torch.float8_e4m3fn), scales=scales, s=total)
+        dy, t = s["dy"].float(), total.float()
+        rho = torch.rsqrt((t * t).mean(-1, keepdim=True) + EPS)
+        gy = dy * s["w"]
+        c = (gy * t).mean(-1, keepdim=True)
+        dx = s["ds"].float() + rho * gy - rho * rho * rho * c * t
+        return dict(y=y.to(T), s=total, dx=dx.to(T), dw=(dy * t * rho).sum(0))
+    if k == "conv":
+        W, L = case["taps"], case["length"]
+        ok = _valid(s, L)
+        x = s["x"].float()
+        xp = torch.nn.functional.pad(x, (0, 0, W - 1, 0))
+        win = xp.unfold(1, W, 1)                                        # [B, L, D, W]
+        p = (win * s["w"]).sum(-1) + s["b"]
+        y = torch.where(ok, _silu(p), 0).to(T)
+        if not case["train"]:
+            at = s["lengths"].long()[:, None] + torch.arange(W - 1, device="cuda")
+            return dict(y=y, state=xp.gather(1, at[..., None].expand(-1, -1, x.shape[2])).to(T))
+        dp = torch.where(ok, s["dy"].float() * _dsilu(p), 0)
+        dx = (torch.nn.functional.pad(dp, (0, 0, 0, W - 1)).unfold(1, W, 1) * s["w"].flip(1)).sum(-1)
+        return dict(y=y, dx=dx.to(T), dw=(dp[..., None] * win).sum((0, 1)), db=dp.sum((0, 1)))
+    if k == "scan":
+        L, D = case["length"], case["channels"]
+        ok = _valid(s, L)
+        u, z, raw = s["u"].float(), s["z"].float(), s["delta"].float() + s["bias"]
+        dt = torch.where(ok, _softplus(raw), 0)                         # a step of 0 leaves the state as it is
+        A, Bm, Cm = s["A"], _per_channel(s["B"].float(), D), _per_channel(s["C"].float(), D)
+        a = torch.exp(dt[..., None] * A)
+        h = _linear_scan(a, (dt * u)[..., None] * Bm)
+        yt = (h * Cm).sum(-1) + s["D"] * u
+        y = torch.where(ok, yt * _silu(z), 0).to(T)
+        if not case["train"]:
+            return dict(y=y, state=h[:, -1].clone())
+        dout = torch.where(ok, s["dy"].float(), 0)
+        dyt, dz = dout * _silu(z), dout * yt * _dsilu(z)
+        # the adjoint state: g_t = C_t dy_t + a_{t+1} g_{t+1}
+        nxt = torch.cat((a[:, 1:], torch.zeros_like(a[:, :1])), 1)
+        gr = _linear_scan(nxt.flip(1), (dyt[..., None] * Cm).flip(1)).flip(1)
+        G, N = s["B"].shape[2:]
+        grouped = lambda v: v.view(*v.shape[:2], G, D // G, N).sum(3)  # noqa: E731
+        dC, dB = grouped(h * dyt[..., None]), grouped(gr * (dt * u)[..., None])
+        gB = (gr * Bm).sum(-1)
+        ah = gr * a * torch.cat((torch.zeros_like(h[:, :1]), h[:, :-1]), 1)
+        draw_ = torch.where(ok, ((ah * A).sum(-1) + gB * u) / (1 + torch.exp(-raw)), 0)
+        return dict(y=y, du=(s["D"] * dyt + dt * gB).to(T), ddelta=draw_.to(T), dA=(ah * dt[..., None]).sum((0, 1)),
+                    dB=dB.to(T), dC=dC.to(T), dD=(dyt * u).sum((0, 1)), dz=dz.to(T), dbias=draw_.sum((0, 1)))
+    if k == "step":
+        D = case["channels"]
+        win = torch.cat((s["conv_state"].float(), s["x"].float()[:, None]), 1)      # [B, W, D]
+        c = _silu((win * s["w"].t()).sum(1) + s["b"]).to(T)
+        s["conv_state"].copy_(win[:, 1:])
+        u, dt = c.float(), _softplus(s["delta"].float() + s["bias"])
+        h = s["state"] * torch.exp(dt[..., None] * s["A"]) + (dt * u)[..., None] * _per_channel(s["B"].float(), D)
+        s["state"].copy_(h)
+        y = ((h * _per_channel(s["C"].float(), D)).sum(-1) + s["D"] * u) * _silu(s["z"].float())
+        return dict(c=c, conv_state=s["conv_state"], y=y.to(T), state=s["state"])
+    up = s["G"].float()
+    if k == "muon":
+        s["M"].mul_(MUON["momentum"]).add_(up)
+        up = up + MUON["momentum"] * s["M"]
+    x = up / (torch.sqrt((up * up).sum((1, 2), keepdim=True)) + NS_EPS)
+    tall = case["m"] > case["n"]
+    if tall:
+        x = x.mT.contiguous()
+    ca, cb, cc = NS_COEFFS
+    for _ in range(NS_STEPS):
+        xx = torch.matmul(x, x.mT.contiguous())
+        x = ca * x + torch.matmul(cb * xx + cc * torch.matmul(xx, xx), x)
+    if tall:
+        x = x.mT.contiguous()
+    if k == "ortho":
+        return dict(o=x.to(T))
+    scale = math.sqrt(max(1.0, case["m"] / case["n"]))
+    s["Wt"].copy_(s["Wt"].float() * (1 - MUON["lr"] * MUON["weight_decay"]) - MUON["lr"] * scale * x)
+    return dict(w=s["Wt"], m=s["M"])
+
+
+# ---------------------------------------------------------------------------
+# What a pass cannot do without.
+
+def work(case):
+    e = 4 if case["type"] == "f32" else 2
+    k = case["kind"]
+    if k in ("norm8", "norm"):
+        n, d = case["rows"] * case["width"], case["width"]
+        if k == "norm8":
+            groups = -(-d // (case["group"] or d))
+            return dict(bytes=n * (3 * e + 1) + 4 * (d + case["rows"] * groups), flops=8 * n)
+        return dict(bytes=n * 8 * e + 12 * d, flops=18 * n)
+    if k == "conv":
+        D, W = case["channels"], case["taps"]
+        n = case["batch"] * case["length"] * D
+        par = 4 * D * (W + 1)
+        if not case["train"]:
+            return dict(bytes=2 * n * e + par + case["batch"] * (W - 1) * D * e, flops=n * (2 * W + 5))
+        return dict(bytes=5 * n * e + 3 * par, flops=n * (8 * W + 18))
+    if k == "scan":
+        D, N, G = case["channels"], case["states"], case["groups"]
+        t = case["batch"] * case["length"]
+        n, bc, par = t * D, 2 * t * G * N, 4 * D * (N + 2)
+        if not case["train"]:
+            return dict(bytes=(4 * n + bc) * e + par + 4 * case["batch"] * D * N, flops=n * (7 * N + 12))
+        # forward; backward: the forward's states again, the adjoint states, the gradients
+        return dict(bytes=(4 * n + bc) * e + par + (7 * n + 2 * bc) * e + 2 * par, flops=n * (26 * N + 40))
+    if k == "step":
+        B, D, N, W = case["batch"], case["channels"], case["states"], case["taps"]
+        n = B * D
+        return dict(bytes=n * (8 * N + e * (5 + 2 * (W - 1))) + 2 * B * case["groups"] * N * e + 4 * D * (N + W + 3),
+                    flops=n * (7 * N + 2 * W + 20))
+    lo, hi = sorted((case["m"], case["n"]))
+    n = case["count"] * lo * hi
+    # the two symmetric products need one triangle each
+    flops = case["count"] * NS_STEPS * (lo * (lo + 1) * hi + lo * (lo + 1) * lo + 2 * lo * lo * hi)
+    return dict(bytes=n * (2 * e if k == "ortho" else 3 * e + 8), flops=flops)
+
+
+# ---------------------------------------------------------------------------
+# The same outputs in 64 bits, from the definitions: sequences level by level.
+
+def exact(case, seed):
+    s = {k: v.double() if isinstance(v, torch.Tensor) and v.is_floating_point() else v
+         for k, v in prepare(case, seed).items()}
+    return {"norm8": _exact_norm, "norm": _exact_norm, "conv": _exact_conv, "scan": _exact_scan, "step": _exact_step,
+            "muon": _exact_muon, "ortho": _exact_muon}[case["kind"]](case, s)
+
+
+def _exact_norm(case, s):
+    t = s["x"] + s["r"]
+    rms = (t.pow(2).sum(1, keepdim=True) / case["width"] + EPS).sqrt()
+    unit = t / rms
+    y = unit * s["w"]
+    if case["kind"] == "norm8":
+        step = case["group"] or case["width"]
+        parts = y.split(step, 1)
+        scales = torch.stack([p.abs().max(1).values for p in parts], 1) / F8_MAX
+        return dict(q=None, scales=scales, s=t)
+    # y = w t / rms with rms^2 = t.t / d + eps:  dy/dt = w (1 - unit unit^T / d) / rms
+    v = s["dy"] * s["w"]
+    dx = s["ds"] + (v - unit * (v * unit).sum(1, keepdim=True) / case["width"]) / rms
+    return dict(y=y, s=t, dx=dx, dw=(s["dy"] * unit).sum(0))
+
+
+def _inside(s, t):
+    return (s["lengths"] > t)[:, None]
+
+
+def _exact_conv(case, s):
+    W, L = case["taps"], case["length"]
+    x, w, n = s["x"], s["w"], s["lengths"]
+    p = s["b"].expand_as(x).clone()
+    for lag in range(min(W, L)):
+        p[:, lag:] += w[:, W - 1 - lag] * x[:, :L - lag]
+    sig = torch.sigmoid(p)
+    ok = (torch.arange(L, device="cuda") < n[:, None])[..., None]
+    y = p * sig * ok
+    if not case["train"]:
+        last = torch.zeros(case["batch"], W - 1, case["channels"], dtype=torch.float64, device="cuda")
+        for i in range(W - 1):
+            at = n.long() - (W - 1) + i
+            rows = x[torch.arange(case["batch"], device="cuda"), at.clamp(min=0)]
+            last[:, i] = rows * (at >= 0)[:, None]
+        return dict(y=y, state=last)
+    dp = s["dy"] * sig * (1 + p * (1 - sig)) * ok
+    dx, dw = torch.zeros_like(x), torch.zeros_like(w)
+    for lag in range(min(W, L)):
+        dx[:, :L - lag] += w[:, W - 1 - lag] * dp[:, lag:]
+        dw[:, W - 1 - lag] = (dp[:, lag:] * x[:, :L - lag]).sum((0, 1))
+    return dict(y=y, dx=dx, dw=dw, db=dp.sum((0, 1)))
+
+
+def _exact_scan(case, s):
+    L, D, G = case["length"], case["channels"], case["groups"]
+    per = D // G
+    A, u, z, d0 = s["A"], s["u"], s["z"], s["D"]
+    raw = s["delta"] + s["bias"]
+    dt = torch.nn.functional.softplus(raw, threshold=60.0)
+    group = torch.arange(D, device="cuda") // per
+    h = torch.zeros(case["batch"], *A.shape, dtype=torch.float64, device="cuda")
+    y, keep = torch.zeros_like(u), []
+    for t in range(L):
+        new = torch.exp(dt[:, t, :, None] * A) * h + (dt[:, t] * u[:, t])[..., None] * s["B"][:, t, group]
+        h = torch.where(_inside(s, t)[..., None], new, h)
+        y[:, t] = (h * s["C"][:, t, group]).sum(-1) + d0 * u[:, t]
+        if case["train"]:
+            keep.append(h)
+    sig = torch.sigmoid(z)
+    ok = (torch.arange(L, device="cuda") < s["lengths"][:, None])[..., None]
+    out = dict(y=y * z * sig * ok)
+    if not case["train"]:
+        return dict(out, state=h)
+    dout = s["dy"] * ok
+    dyt = dout * z * sig
+    out["dz"] = dout * y * sig * (1 + z * (1 - sig))
+    du, ddt = d0 * dyt, torch.zeros_like(u)
+    dA, dB, dC = torch.zeros_like(A), torch.zeros_like(s["B"]), torch.zeros_like(s["C"])
+    lam = torch.zeros_like(h)                       # dL/dh_t
+    for t in reversed(range(L)):
+        lam = lam + dyt[:, t, :, None] * s["C"][:, t, group]
+        dC[:, t] = (keep[t] * dyt[:, t, :, None]).view(-1, G, per, A.shape[1]).sum(2)
+        here = torch.where(_inside(s, t)[..., None], lam, 0.0)
+        dB[:, t] = (here * (dt[:, t] * u[:, t])[..., None]).view(-1, G, per, A.shape[1]).sum(2)
+        gb = (here * s["B"][:, t, group]).sum(-1)
+        du[:, t] += dt[:, t] * gb
+        decay = torch.exp(dt[:, t, :, None] * A)
+        moved = here * decay * keep[t - 1] if t else torch.zeros_like(here)
+        ddt[:, t] = (moved * A).sum(-1) + gb * u[:, t]
+        dA += (moved * dt[:, t, :, None]).sum(0)
+        lam = torch.where(_inside(s, t)[..., None], lam * decay, lam)
+    ddelta = ddt * torch.sigmoid(raw)
+    out.update(du=du, ddelta=ddelta, dA=dA, dB=dB, dC=dC, dD=(dyt * u).sum((0, 1)), dbias=ddelta.sum((0, 1)))
+    return out
+
+
+def _exact_step(case, s):
+    W, per = case["taps"], case["channels"] // case["groups"]
+    p = s["b"] + s["w"][:, W - 1] * s["x"]
+    for i in range(W - 1):
+        p = p + s["w"][:, i] * s["conv_state"][:, i]
+    c = p * torch.sigmoid(p)
+    group = torch.arange(case["channels"], device="cuda") // per
+    # the scan reads the convolution's output as it is stored
+    u = c.to(TYPES[case["type"]]).double()
+    dt = torch.nn.functional.softplus(s["delta"] + s["bias"], threshold=60.0)
+    h = torch.exp(dt[..., None] * s["A"]) * s["state"] + (dt * u)[..., None] * s["B"][:, group]
+    y = ((h * s["C"][:, group]).sum(-1) + s["D"] * u) * s["z"] * torch.sigmoid(s["z"])
+    return dict(c=c, conv_state=torch.cat((s["conv_state"], s["x"][:, None]), 1)[:, 1:], y=y, state=h)
+
+
+def _exact_muon(case, s):
+    a, b, c = NS_COEFFS
+    outs, moms = [], []
+    for i in range(case["count"]):
+        up = s["G"][i]
+        if case["kind"] == "muon":
+            moms.append(MUON["momentum"] * s["M"][i] + up)
+            up = up + MUON["momentum"] * moms[-1]
+        x = up / (torch.linalg.norm(up) + NS_EPS)
+        for _ in range(NS_STEPS):
+            # the same polynomial from the right or the left, whichever is smaller
+            if case["m"] > case["n"]:
+                k = torch.mm(x.t().contiguous(), x)
+                x = a * x + torch.mm(x, b * k + c * torch.mm(k, k))
+            else:
+                k = torch.mm(x, x.t().contiguous())
+                x = a * x + torch.mm(b * k + c * torch.mm(k, k), x)
+        outs.append(x)
+    o = torch.stack(outs)
+    if case["kind"] == "ortho":
+        return dict(o=o)
+    scale = max(1.0, case["m"] / case["n"]) ** 0.5
+    return dict(w=s["Wt"] * (1 - MUON["lr"] * MUON["weight_decay"]) - MUON["lr"] * scale * o, m=torch.stack(moms))
