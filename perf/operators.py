@@ -29,33 +29,33 @@ F8_TINY = 2.0 ** -126                   # smallest scale of a group
 def listed():
     return [
         # one time level of 64 nodes of a rollout enters a block in 8 bits
-        dict(name="norm f8, 64 x 256", kind="norm8", rows=64, width=256, type="bf16", group=128),
+        dict(name="norm f8 64 x 256", kind="norm8", rows=64, width=256, type="bf16", group=128),
         # a surrogate's activations over part of a grid, odd row count, ragged last group
-        dict(name="norm f8, 50021 x 1160", kind="norm8", rows=50021, width=1160, type="bf16", group=128),
+        dict(name="norm f8 50021 x 1160", kind="norm8", rows=50021, width=1160, type="bf16", group=128),
         # training on the Burgers grid (128 x 256 nodes), the widest network of the paper
-        dict(name="norm train, 32768 x 256", kind="norm", rows=32768, width=256, type="f32"),
+        dict(name="norm train 32768 x 256", kind="norm", rows=32768, width=256, type="f32"),
         # training on the Helmholtz grid (1024 x 1024 nodes)
-        dict(name="norm train, 1048576 x 128", kind="norm", rows=1048576, width=128, type="bf16"),
+        dict(name="norm train 1048576 x 128", kind="norm", rows=1048576, width=128, type="bf16"),
         # the Burgers grid as 256 sequences of 128 time levels, twice the widest network's channels
-        dict(name="conv train, 256 x 128 x 512", kind="conv", train=True, batch=256, length=128, channels=512,
+        dict(name="conv train 256 x 128 x 512", kind="conv", train=True, batch=256, length=128, channels=512,
              taps=4, type="bf16"),
         # a prompt of odd lengths, three taps
-        dict(name="conv prompt, 3 x 1021 x 200", kind="conv", train=False, batch=3, length=1021, channels=200,
+        dict(name="conv prompt 3 x 1021 x 200", kind="conv", train=False, batch=3, length=1021, channels=200,
              taps=3, type="f32"),
         # a long prompt: a 128 x 128 grid's nodes in scan order, few sequences
-        dict(name="scan prompt, 2 x 16384 x 512", kind="scan", train=False, batch=2, length=16384, channels=512,
+        dict(name="scan prompt 2 x 16384 x 512", kind="scan", train=False, batch=2, length=16384, channels=512,
              states=16, groups=1, type="f32"),
         # training on long windows
-        dict(name="scan train, 8 x 2048 x 1024", kind="scan", train=True, batch=8, length=2048, channels=1024,
+        dict(name="scan train 8 x 2048 x 1024", kind="scan", train=True, batch=8, length=2048, channels=1024,
              states=16, groups=1, type="bf16"),
         # one time level of a rollout at 256 nodes: convolution and scan with their carried states
-        dict(name="step, 256 x 512", kind="step", batch=256, channels=512, states=16, groups=1, taps=4, type="bf16"),
+        dict(name="step 256 x 512", kind="step", batch=256, channels=512, states=16, groups=1, taps=4, type="bf16"),
         # the update of a network of the paper's width 128
-        dict(name="muon, 6 of 128 x 128", kind="muon", count=6, m=128, n=128, type="f32"),
+        dict(name="muon 6 of 128 x 128", kind="muon", count=6, m=128, n=128, type="f32"),
         # in and out projections of a small block, not square
-        dict(name="orthogonalize, 4 of 260 x 1000", kind="ortho", count=4, m=260, n=1000, type="f32"),
+        dict(name="orthogonalize 4 of 260 x 1000", kind="ortho", count=4, m=260, n=1000, type="f32"),
         # one large matrix in 16 bits
-        dict(name="muon, 4096 x 4096", kind="muon", count=1, m=4096, n=4096, type="bf16"),
+        dict(name="muon 4096 x 4096", kind="muon", count=1, m=4096, n=4096, type="bf16"),
     ]
 
 
