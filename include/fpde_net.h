@@ -1,0 +1,175 @@
+/*
+ * fpde_net.h -- C ABI of libfpde_net: the operators of a time-marching network
+ * whose output fields the residual operators of fpde.h judge, for AMD Instinct
+ * MI355X (gfx950).
+ *
+ *   fpde_rms_norm          root-mean-square norm with the residual stream's
+ *                          addition; output in the data's type or in 8 bits
+ *   fpde_rms_norm_bwd      its gradients
+ *   fpde_causal_conv       short causal convolution along time, with the state
+ *                          that carries it from one window (or level) to the next
+ *   fpde_causal_conv_bwd   its gradients
+ *   fpde_selective_scan    selective state space scan along time: whole windows
+ *                          (ragged), or one level from a carried state
+ *   fpde_selective_scan_bwd  its gradients
+ *   fpde_orthogonalize     Newton-Schulz orthogonalisation of matrices
+ *   fpde_muon_step         momentum, orthogonalised update and weights in one call
+ *
+ * Common rules:
+ *   - Arguments come in one struct, in host memory, read during the call.  Its
+ *     pointers are DEVICE pointers unless said otherwise, aligned to their
+ *     element (FPDE_ERR_ALIGN), allocated on the current HIP device; the last axis
+ *     of every array is dense.  Strides are in elements.
+ *   - The caller owns every buffer, the workspace too, and keeps it alive until
+ *     the work queued on `stream` has completed.  The library allocates nothing
+ *     and keeps no state; calls are reentrant, and may be captured in a graph.
+ *   - A workspace needs no preparation and holds nothing between calls; calls that
+ *     may run at the same time need one each.  16-byte aligned; the functions
+ *     ending in _workspace give its size in bytes (0: none is needed and it may be
+ *     NULL; a negative value is the status of arguments that the call refuses).
+ *   - `stream` is a hipStream_t (NULL: the default stream).  All work is queued on
+ *     it; the host never synchronises.
+ *   - Arguments are validated on the host before anything is queued; on any error
+ *     the call returns a negative fpde_status and queues nothing (FPDE_ERR_HIP
+ *     apart: a launch that failed may follow others of the same call).
+ *   - Outputs overlap no other buffer of the call (FPDE_ERR_ARG), except where a
+ *     struct member says that it may be another one, updated in place.
+ *   - Sums, statistics and states are float32 or wider; results are rounded once,
+ *     to nearest even, when they are stored.  Results do not depend on timing: no
+ *     atomics, every sum in a fixed order.
+ *   - NaN and Inf in the data are not checked; they propagate.
+ */
+#ifndef FPDE_NET_H
+#define FPDE_NET_H
+
+#include <stdint.h>
+
+#include "fpde.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* Element types.  The data of one call has one of the first three. */
+typedef enum fpde_dtype {
+    FPDE_F32 = 0,
+    FPDE_BF16 = 1,
+    FPDE_F16 = 2,
+    FPDE_F8E4M3 = 3 /* output of fpde_rms_norm only: 1-4-3 bits, no infinities, largest value 448 */
+} fpde_dtype;
+
+/* ---------------------------------------------------------------------------
+ * Root-mean-square norm with the residual stream's addition:
+ *     s = x + residual,  y = weight * s / sqrt(mean(s^2) + eps),
+ * the mean over a row's `width` columns.  y is formed from the unrounded s.
+ *
+ * Output in 8 bits (out_dtype FPDE_F8E4M3): each group of `group` columns
+ * (128; the last group of a row may be shorter; 0: the whole row) has the scale
+ *     sigma = max(max|y| / 448, 2^-126),
+ * and holds e4m3(y / sigma), so that y is about sigma * q.  A NaN in y stays a
+ * NaN in q and does not enter sigma.
+ *
+ * Limits: 0 <= rows <= 2^40, 1 <= width <= 2^20 (FPDE_ERR_SHAPE); row strides of
+ * at least width. */
+typedef struct fpde_norm_args {
+    int32_t dtype;            /* x, residual, sum and (unless 8 bits) y */
+    int32_t weight_dtype;     /* FPDE_F32, or dtype */
+    int32_t out_dtype;        /* dtype, or FPDE_F8E4M3 */
+    int32_t group;            /* 8 bits: 128, or 0 for the row */
+    int64_t rows, width;
+    int64_t x_stride, residual_stride; /* from row to row */
+    double eps;               /* >= 0 and finite (FPDE_ERR_COEFF) */
+    const void* x;
+    const void* residual;     /* or NULL: s = x */
+    const void* weight;       /* [width], or NULL: ones */
+    void* y;                  /* [rows][width] */
+    void* sum;                /* [rows][width]: s rounded to dtype; or NULL.  May be `x` or
+                                 `residual` themselves if that is dense (updated in place) */
+    float* scales;            /* 8 bits: [rows][ceil(width / group)] ([rows][1] for group 0) */
+} fpde_norm_args;
+
+int fpde_rms_norm(const fpde_norm_args* a, void* stream);
+
+/* Gradients of fpde_rms_norm.  With rho = 1 / sqrt(mean(sum^2) + eps), g = weight * dy:
+ *     ds = dsum + rho * g - rho^3 * mean(g * sum) * sum   (of x and of residual alike)
+ *     dweight = sum over rows of dy * sum * rho
+ * `sum` is what the forward wrote (or x where it had no residual). */
+typedef struct fpde_norm_bwd_args {
+    int32_t dtype;            /* dy, sum, dsum, ds */
+    int32_t weight_dtype;     /* weight and dweight: FPDE_F32, or dtype */
+    int64_t rows, width;
+    int64_t dy_stride, sum_stride, dsum_stride;
+    double eps;
+    const void* dy;
+    const void* sum;
+    const void* dsum;         /* gradient that reaches s by the residual stream, or NULL: zero */
+    const void* weight;       /* or NULL: ones */
+    void* ds;                 /* [rows][width]; may be `dy` or `dsum` itself if that is dense */
+    void* dweight;            /* [width]; NULL if and only if it is not wanted */
+    void* workspace;
+    int64_t workspace_bytes;
+} fpde_norm_bwd_args;
+
+int64_t fpde_rms_norm_bwd_workspace(const fpde_norm_bwd_args* a); /* (reads sizes, types, dweight's presence) */
+int fpde_rms_norm_bwd(const fpde_norm_bwd_args* a, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Short causal convolution along time, one filter per channel:
+ *     p[b][t][c] = bias[c] + sum_k weight[c][k] * x[b][t - taps + 1 + k][c],
+ *     y = p, or p * sigmoid(p) with `silu`.
+ * x at t < 0 is the carried state: state[b][taps - 1 + t][c], or zero without one.
+ * Sequence b holds lengths[b] levels (NULL: `length`; values are clamped to 0 ..
+ * length): y is 0 past them and x there is not read.  state_out gets the last
+ * taps - 1 levels of each sequence, state included where it is shorter.  A single
+ * level (length 1) with state_out = state is the step of a rollout.
+ *
+ * Limits: 2 <= taps <= 4, 1 <= channels <= 2^20, 0 <= batch, 0 <= length < 2^31,
+ * batch * length <= 2^40. */
+typedef struct fpde_conv_args {
+    int32_t dtype;            /* x, y, state, state_out */
+    int32_t weight_dtype;     /* weight and bias: FPDE_F32, or dtype */
+    int32_t taps;
+    int32_t silu;             /* 0 or 1 */
+    int64_t batch, length, channels;
+    int64_t x_batch_stride, x_time_stride;
+    const void* x;
+    const void* weight;       /* [channels][taps] */
+    const void* bias;         /* [channels] or NULL */
+    const void* state;        /* [batch][taps - 1][channels] or NULL */
+    const int32_t* lengths;   /* [batch] or NULL */
+    void* y;                  /* [batch][length][channels] */
+    void* state_out;          /* [batch][taps - 1][channels] or NULL; may be `state` */
+} fpde_conv_args;
+
+int fpde_causal_conv(const fpde_conv_args* a, void* stream);
+
+/* Gradients of fpde_causal_conv; the carried state is data (no gradient goes
+ * through it).  dx is 0 past a sequence's levels, where dy is not read. */
+typedef struct fpde_conv_bwd_args {
+    int32_t dtype;
+    int32_t weight_dtype;     /* weight, bias, dweight, dbias */
+    int32_t taps;
+    int32_t silu;
+    int64_t batch, length, channels;
+    int64_t x_batch_stride, x_time_stride;
+    int64_t dy_batch_stride, dy_time_stride;
+    const void* dy;
+    const void* x;
+    const void* weight;
+    const void* bias;
+    const void* state;
+    const int32_t* lengths;
+    void* dx;                 /* [batch][length][channels] */
+    void* dweight;            /* [channels][taps] */
+    void* dbias;              /* [channels]; NULL if and only if not wanted */
+    void* workspace;
+    int64_t workspace_bytes;
+} fpde_conv_bwd_args;
+
+int64_t fpde_causal_conv_bwd_workspace(const fpde_conv_bwd_args* a); /* (reads sizes and types) */
+int fpde_causal_conv_bwd(const fpde_conv_bwd_args* a, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* FPDE_NET_H */

@@ -6,16 +6,20 @@ kernels in ``csrc/`` and exposed here through a thin ctypes binding:
 ``fpde_residual_bwd`` (interior analytic adjoint, gather form) and
 ``fpde_bc_correct`` (boundary-gradient correction).  ``workloads`` holds the
 seeded synthetic inputs of the five benchmark operators.
+
+``network`` holds the operators of the networks whose fields the residuals
+judge (include/fpde_net.h): norm, causal convolution and selective scan along
+time, orthogonalised weight updates.
 """
 from . import workloads  # noqa: F401
 
-__all__ = ["workloads", "binding"]
+__all__ = ["workloads", "binding", "network"]
 
 
 def __getattr__(name):
-    # the binding loads libfpde.so; import it lazily so that the workload
-    # generators stay usable on machines without the built library
-    if name == "binding":
+    # the bindings load the built libraries; import them lazily so that the workload
+    # generators stay usable on machines without them
+    if name in ("binding", "network"):
         import importlib  # noqa: PLC0415
-        return importlib.import_module(".binding", __name__)
+        return importlib.import_module("." + name, __name__)
     raise AttributeError(name)

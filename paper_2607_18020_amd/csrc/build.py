@@ -1,7 +1,8 @@
 """Build libfpde.so (gfx950) in-tree with hipcc.
 
 Usage: python -m paper_2607_18020_amd.csrc.build [--save-temps]
-Writes paper_2607_18020_amd/libfpde.so.  Packed-FP32 VALU ops are disabled
+Writes paper_2607_18020_amd/libfpde.so (and its checking build) and
+libfpde_net.so, the network operators.  Packed-FP32 VALU ops are disabled
 for all device code; float64 atomics use the native global_atomic_add_f64;
 floating-point contraction is off (the operators' fmaf are explicit).
 """
@@ -10,6 +11,7 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 PKG = os.path.dirname(HERE)
@@ -51,6 +53,12 @@ CHECK_FLAGS = [
     "-DFPDE_BWD2_QUEUE=0",
 ]
 
+# The network operators (include/fpde_net.h): one object per source, compiled in
+# parallel, in a library of its own.
+NET_LIB = os.path.join(PKG, "libfpde_net.so")
+NET_DIR = os.path.join(HERE, "net")
+NET_SOURCES = [os.path.join(NET_DIR, f) for f in ("norm.hip", "conv.hip")]
+
 _NOISE = "is not a recognized feature for this target"
 
 
@@ -72,10 +80,29 @@ def _finish(p, out: str, verbose: bool) -> None:
     os.replace(out + ".tmp", out)
 
 
+def build_net(verbose: bool = False, out: str = NET_LIB) -> str:
+    """Compile the network operators' library."""
+    flags = [f for f in FLAGS if f != "-shared"] + ["-I", NET_DIR, "-c"]
+    with tempfile.TemporaryDirectory(prefix="fpde_net_") as tmp:
+        procs, objects = [], []
+        for src in NET_SOURCES:
+            obj = os.path.join(tmp, os.path.basename(src) + ".o")
+            cmd = [HIPCC, *flags, "-o", obj + ".tmp", src]
+            if verbose:
+                print(" ".join(cmd), flush=True)
+            objects.append(obj)
+            procs.append(subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.PIPE, text=True))
+        for p, obj in zip(procs, objects):
+            _finish(p, obj, verbose)
+        cmd = [HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", out + ".tmp", *objects]
+        _finish(subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.PIPE, text=True), out, verbose)
+    return out
+
+
 def build(save_temps: bool = False, verbose: bool = False, out: str = LIB, extra=(),
           check: bool = True) -> str:
-    """Compile the product library (and, with check, the checking library in
-    parallel)."""
+    """Compile the product library (and, with check, the checking library and the
+    network operators' in parallel)."""
     jobs = [(out, _command(out, extra, save_temps))]
     if check and out == LIB and not extra:
         jobs.append((CHECK_LIB, _command(CHECK_LIB, CHECK_FLAGS)))
@@ -86,8 +113,12 @@ def build(save_temps: bool = False, verbose: bool = False, out: str = LIB, extra
         procs.append((o, subprocess.Popen(
             cmd, stdout=subprocess.PIPE, stderr=subprocess.PIPE, text=True,
             cwd=os.path.join(ROOT, "_build") if save_temps and o == out else None)))
-    for o, p in procs:
-        _finish(p, o, verbose)
+    try:
+        if check and out == LIB and not extra:
+            build_net(verbose)
+    finally:
+        for o, p in procs:
+            _finish(p, o, verbose)
     return out
 
 

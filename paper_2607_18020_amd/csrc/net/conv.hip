@@ -1,0 +1,357 @@
+// conv.hip -- short causal convolution along time, per channel, and its gradients.
+//
+//   p_t = b + sum_k w_k x_{t - W + 1 + k},  y = p or silu(p) = p sigmoid(p)
+//   dp = dy (silu'(p) = q (1 + p (1 - q)), q = sigmoid(p));  dx_t = sum_k w_k dp_{t + W - 1 - k}
+//   dw_k = sum_t dp_t x_{t - W + 1 + k},  db = sum_t dp_t
+//
+// A lane owns the channels of one 16-byte load and marches a chunk of levels,
+// the last W - 1 of them in registers, so x is read once but for the W - 1 levels
+// before a chunk; the loads of kBlock levels are in flight together.  What bounds
+// both directions is memory.  The backward recomputes p from x instead of
+// reading it, and runs W - 1 levels past its chunk for the dp that dx needs there.
+#include "net_common.hpp"
+
+using namespace fpde_net;
+
+namespace {
+
+constexpr int kBlock = 8;    // levels whose loads are in flight together
+constexpr int kFwdChunk = 32;
+constexpr int kBwdChunk = 64;
+
+struct ConvP {
+    const void *x, *dy, *w, *b, *state;
+    const int32_t* lengths;
+    void *y, *state_out;  // y: dx in the backward
+    float *dw, *db;       // partials [slots][channels * taps], [slots][channels]
+    int64_t batch, chunks, xb, xt, dyb, dyt;
+    int length, channels, wf32, silu;
+};
+
+__device__ __forceinline__ int levels(const ConvP& P, int64_t b) {
+    if (!P.lengths) return P.length;
+    const int n = P.lengths[b];
+    return n < 0 ? 0 : (n < P.length ? n : P.length);
+}
+
+// x at level t of sequence b, which holds len: its own levels, the carried state before
+// them, or zero
+template <class T, int W, int V>
+__device__ __forceinline__ void x_at(const ConvP& P, int64_t b, int t, int len, int c, int n,
+                                     float (&v)[V]) {
+    if (t >= 0 && t < len)
+        load_f32<T, V>(v, (const T*)P.x + b * P.xb + (int64_t)t * P.xt + c, n);
+    else if (t < 0 && P.state)
+        load_f32<T, V>(v, (const T*)P.state + (b * (W - 1) + (W - 1 + t)) * P.channels + c, n);
+    else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = 0.f;
+    }
+}
+
+// the filters of V channels: w[k][i], and the bias
+template <class T, int W, int V>
+__device__ __forceinline__ void load_filters(const ConvP& P, int c, int n, float (&w)[W][V], float (&b)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+#pragma unroll
+        for (int k = 0; k < W; ++k)
+            w[k][i] = i < n ? param<T>(P.w, P.wf32, (int64_t)(c + i) * W + k) : 0.f;
+        b[i] = P.b && i < n ? param<T>(P.b, P.wf32, c + i) : 0.f;
+    }
+}
+
+template <class T, int W>
+__global__ __launch_bounds__(64) void conv_fwd_kernel(ConvP P) {
+    constexpr int V = kVec<T>;
+    const int c = ((int)blockIdx.x * 64 + (int)threadIdx.x) * V, n = P.channels - c;
+    if (n <= 0) return;
+    float w[W][V], bias[V];
+    load_filters<T, W, V>(P, c, n, w, bias);
+    for (int64_t job = blockIdx.y; job < P.batch * P.chunks; job += gridDim.y) {
+        const int64_t b = job / P.chunks;
+        const int t0 = (int)(job - b * P.chunks) * kFwdChunk, len = levels(P, b);
+        const int t1 = t0 + kFwdChunk < P.length ? t0 + kFwdChunk : P.length;
+        float win[W][V];  // win[k]: x at t - W + 1 + k
+#pragma unroll
+        for (int k = 0; k < W - 1; ++k) x_at<T, W, V>(P, b, t0 - (W - 1) + k, len, c, n, win[k + 1]);
+        if (t0 == 0 && P.state_out) {
+            // The lane that reads the state is the one that replaces it, after its reads.
+            float last[W - 1][V];
+#pragma unroll
+            for (int i = 0; i < W - 1; ++i) x_at<T, W, V>(P, b, len - (W - 1) + i, len, c, n, last[i]);
+#pragma unroll
+            for (int i = 0; i < W - 1; ++i)
+                store_f32<T, V>((T*)P.state_out + (b * (W - 1) + i) * P.channels + c, last[i], n);
+        }
+        T* y = (T*)P.y + (b * P.length + t0) * P.channels + c;
+        for (int t = t0; t < t1; t += kBlock) {
+            float x[kBlock][V];
+#pragma unroll
+            for (int j = 0; j < kBlock; ++j)
+                if (t + j < len && t + j < t1)
+                    load_f32<T, V>(x[j], (const T*)P.x + b * P.xb + (int64_t)(t + j) * P.xt + c, n);
+#pragma unroll
+            for (int j = 0; j < kBlock; ++j) {
+                if (t + j >= t1) break;
+                float p[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) p[i] = 0.f;
+                if (t + j < len) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        p[i] = bias[i];
+#pragma unroll
+                        for (int k = 0; k < W - 1; ++k) {
+                            win[k][i] = win[k + 1][i];
+                            p[i] = fmaf(w[k][i], win[k][i], p[i]);
+                        }
+                        win[W - 1][i] = x[j][i];
+                        p[i] = fmaf(w[W - 1][i], x[j][i], p[i]);
+                        if (P.silu) p[i] = silu(p[i]);
+                    }
+                }
+                store_f32<T, V>(y + (int64_t)(t - t0 + j) * P.channels, p, n);
+            }
+        }
+    }
+}
+
+template <class T, int W>
+__global__ __launch_bounds__(64) void conv_bwd_kernel(ConvP P) {
+    constexpr int V = kVec<T>;
+    const int c = ((int)blockIdx.x * 64 + (int)threadIdx.x) * V, n = P.channels - c;
+    if (n <= 0) return;
+    float w[W][V], bias[V], dw[W][V], db[V];
+    load_filters<T, W, V>(P, c, n, w, bias);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        db[i] = 0.f;
+#pragma unroll
+        for (int k = 0; k < W; ++k) dw[k][i] = 0.f;
+    }
+    for (int64_t job = blockIdx.y; job < P.batch * P.chunks; job += gridDim.y) {
+        const int64_t b = job / P.chunks;
+        const int t0 = (int)(job - b * P.chunks) * kBwdChunk, len = levels(P, b);
+        const int t1 = t0 + kBwdChunk < P.length ? t0 + kBwdChunk : P.length;
+        float win[W][V];  // win[k]: x at t - W + 1 + k
+        float dps[W][V];  // dps[k]: dp at t - W + 1 + k
+#pragma unroll
+        for (int k = 0; k < W - 1; ++k) {
+            x_at<T, W, V>(P, b, t0 - (W - 1) + k, len, c, n, win[k + 1]);
+#pragma unroll
+            for (int i = 0; i < V; ++i) dps[k + 1][i] = 0.f;
+        }
+        T* dx = (T*)P.y + (b * P.length) * P.channels + c;
+        // dx at level t - W + 1 is complete with dp at t: W - 1 levels more than the chunk has
+        for (int t = t0; t < t1 + W - 1; t += kBlock) {
+            float x[kBlock][V], g[kBlock][V];
+#pragma unroll
+            for (int j = 0; j < kBlock; ++j)
+                if (t + j < len && t + j < t1 + W - 1) {
+                    load_f32<T, V>(x[j], (const T*)P.x + b * P.xb + (int64_t)(t + j) * P.xt + c, n);
+                    load_f32<T, V>(g[j], (const T*)P.dy + b * P.dyb + (int64_t)(t + j) * P.dyt + c, n);
+                }
+#pragma unroll
+            for (int j = 0; j < kBlock; ++j) {
+                if (t + j >= t1 + W - 1) break;
+                const bool own = t + j < t1;  // (the levels past the chunk count in the next one's dw)
+                float d[V];
+                if (t + j < len) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        float p = bias[i];
+#pragma unroll
+                        for (int k = 0; k < W - 1; ++k) {
+                            win[k][i] = win[k + 1][i];
+                            p = fmaf(w[k][i], win[k][i], p);
+                        }
+                        win[W - 1][i] = x[j][i];
+                        p = fmaf(w[W - 1][i], x[j][i], p);
+                        d[i] = g[j][i];
+                        if (P.silu) {
+                            const float q = sigmoid(p);
+                            d[i] *= q * fmaf(p, 1.f - q, 1.f);
+                        }
+                        const float o = own ? d[i] : 0.f;
+                        db[i] += o;
+#pragma unroll
+                        for (int k = 0; k < W; ++k) dw[k][i] = fmaf(o, win[k][i], dw[k][i]);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) d[i] = 0.f;
+                }
+                float o[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    o[i] = 0.f;
+#pragma unroll
+                    for (int k = 0; k < W - 1; ++k) dps[k][i] = dps[k + 1][i];
+                    dps[W - 1][i] = d[i];
+                    // dx_s = sum_k w_k dp_{s + W - 1 - k}, s = t - W + 1
+#pragma unroll
+                    for (int k = 0; k < W; ++k) o[i] = fmaf(w[k][i], dps[W - 1 - k][i], o[i]);
+                }
+                const int s = t + j - (W - 1);
+                if (s >= t0) {
+                    if (s >= len) {
+#pragma unroll
+                        for (int i = 0; i < V; ++i) o[i] = 0.f;
+                    }
+                    store_f32<T, V>(dx + (int64_t)s * P.channels, o, n);
+                }
+            }
+        }
+    }
+    float* pw = P.dw + (int64_t)blockIdx.y * P.channels * W + (int64_t)c * W;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+        if (i < n) {
+#pragma unroll
+            for (int k = 0; k < W; ++k) pw[i * W + k] = dw[k][i];
+        }
+    if (P.db) store_f32<float, V>(P.db + (int64_t)blockIdx.y * P.channels + c, db, n);
+}
+
+// ---------------------------------------------------------------------------
+// Host side.
+
+constexpr int64_t kMaxChannels = 1 << 20, kMaxLevels = (int64_t)1 << 40;
+// Wavefronts of a launch before they loop over chunks.  The backward's partial
+// sums grow with them.
+constexpr int64_t kFwdWaves = 1 << 20, kBwdWaves = 8192;
+
+int check_conv(int dtype, int wdtype, int taps, int act, int64_t batch, int64_t length, int64_t channels) {
+    if (size_of(dtype) == 0 || !(wdtype == FPDE_F32 || wdtype == dtype)) return FPDE_ERR_UNSUPPORTED;
+    if (act != 0 && act != 1) return FPDE_ERR_ARG;
+    if (taps < 2 || taps > 4) return FPDE_ERR_UNSUPPORTED;
+    if (batch < 0 || length < 0 || length >= ((int64_t)1 << 31) - 256 || channels < 1 ||
+        channels > kMaxChannels)
+        return FPDE_ERR_SHAPE;
+    if (length > 0 && batch > kMaxLevels / length) return FPDE_ERR_SHAPE;
+    if (batch > kMaxLevels) return FPDE_ERR_SHAPE;
+    return FPDE_OK;
+}
+
+bool strides_ok(int64_t bs, int64_t ts, int64_t batch, int64_t length, int64_t channels) {
+    const int64_t most = (int64_t)1 << 50;
+    if (length > 1 && (ts < channels || ts > most / length)) return false;
+    return batch <= 1 || (bs >= 0 && bs <= most / batch);
+}
+
+int64_t slots(int64_t jobs, int64_t channels, int vec, int64_t waves) {
+    const int64_t n = waves / cdiv(channels, 64 * vec);
+    const int64_t m = n < 1 ? 1 : (n > 65535 ? 65535 : n);
+    return jobs < m ? (jobs < 1 ? 1 : jobs) : m;
+}
+
+// f(T{}, integral_constant<int, taps>)
+template <class F>
+int with_taps(int dtype, int taps, F f) {
+    return with_type(dtype, [&](auto t) {
+        switch (taps) {
+        case 2: return f(t, std::integral_constant<int, 2>{});
+        case 3: return f(t, std::integral_constant<int, 3>{});
+        default: return f(t, std::integral_constant<int, 4>{});
+        }
+    });
+}
+
+}  // namespace
+
+extern "C" int fpde_causal_conv(const fpde_conv_args* a, void* stream) {
+    if (!a) return FPDE_ERR_ARG;
+    int st = check_conv(a->dtype, a->weight_dtype, a->taps, a->silu, a->batch, a->length, a->channels);
+    if (st != FPDE_OK) return st;
+    if (!strides_ok(a->x_batch_stride, a->x_time_stride, a->batch, a->length, a->channels))
+        return FPDE_ERR_SHAPE;
+    if (a->batch == 0 || (a->length == 0 && !a->state_out)) return FPDE_OK;
+    if (!a->weight || (a->length > 0 && (!a->x || !a->y))) return FPDE_ERR_ARG;
+    const int e = size_of(a->dtype), we = size_of(a->weight_dtype);
+    const int64_t hist = a->batch * (a->taps - 1) * a->channels * e;
+    Spans sp;
+    sp.add(a->x, span3(a->batch, a->length, a->channels, a->x_batch_stride, a->x_time_stride, e), e, false);
+    sp.add(a->weight, a->channels * a->taps * we, we, false);
+    sp.add(a->bias, a->channels * we, we, false);
+    sp.add(a->lengths, a->batch * 4, 4, false);
+    sp.add(a->state, hist, e, false);
+    sp.add(a->y, a->batch * a->length * a->channels * e, e, true);
+    sp.add(a->state_out, hist, e, true);
+    st = sp.check(a->state_out, a->state);
+    if (st != FPDE_OK) return st;
+    ConvP P{};
+    P.x = a->x, P.w = a->weight, P.b = a->bias, P.state = a->state, P.lengths = a->lengths;
+    P.y = a->y, P.state_out = a->state_out;
+    P.batch = a->batch, P.xb = a->x_batch_stride, P.xt = a->x_time_stride;
+    P.length = (int)a->length, P.channels = (int)a->channels;
+    P.wf32 = a->weight_dtype == FPDE_F32, P.silu = a->silu;
+    P.chunks = a->length > 0 ? cdiv(a->length, kFwdChunk) : 1;
+    return with_taps(a->dtype, a->taps, [&](auto t, auto w) {
+        using T = decltype(t);
+        const dim3 g((unsigned)cdiv(a->channels, 64 * kVec<T>),
+                     (unsigned)slots(a->batch * P.chunks, a->channels, kVec<T>, kFwdWaves));
+        return launch(conv_fwd_kernel<T, decltype(w)::value>, g, dim3(64), (hipStream_t)stream, P);
+    });
+}
+
+extern "C" int64_t fpde_causal_conv_bwd_workspace(const fpde_conv_bwd_args* a) {
+    if (!a) return FPDE_ERR_ARG;
+    const int st = check_conv(a->dtype, a->weight_dtype, a->taps, a->silu, a->batch, a->length, a->channels);
+    if (st != FPDE_OK) return st;
+    const int64_t jobs = a->batch * cdiv(a->length, kBwdChunk);
+    return slots(jobs, a->channels, 16 / size_of(a->dtype), kBwdWaves) * a->channels * (a->taps + 1) * 4;
+}
+
+extern "C" int fpde_causal_conv_bwd(const fpde_conv_bwd_args* a, void* stream) {
+    if (!a) return FPDE_ERR_ARG;
+    int st = check_conv(a->dtype, a->weight_dtype, a->taps, a->silu, a->batch, a->length, a->channels);
+    if (st != FPDE_OK) return st;
+    if (!strides_ok(a->x_batch_stride, a->x_time_stride, a->batch, a->length, a->channels) ||
+        !strides_ok(a->dy_batch_stride, a->dy_time_stride, a->batch, a->length, a->channels))
+        return FPDE_ERR_SHAPE;
+    const int64_t total = a->batch * a->length;
+    if (!a->weight || !a->dweight || (total > 0 && (!a->x || !a->dy || !a->dx))) return FPDE_ERR_ARG;
+    const int64_t need = fpde_causal_conv_bwd_workspace(a);
+    if (!a->workspace || a->workspace_bytes < need) return FPDE_ERR_ARG;
+    const int e = size_of(a->dtype), we = size_of(a->weight_dtype);
+    Spans sp;
+    sp.add(a->x, span3(a->batch, a->length, a->channels, a->x_batch_stride, a->x_time_stride, e), e, false);
+    sp.add(a->dy, span3(a->batch, a->length, a->channels, a->dy_batch_stride, a->dy_time_stride, e), e, false);
+    sp.add(a->weight, a->channels * a->taps * we, we, false);
+    sp.add(a->bias, a->channels * we, we, false);
+    sp.add(a->lengths, a->batch * 4, 4, false);
+    sp.add(a->state, a->batch * (a->taps - 1) * a->channels * e, e, false);
+    sp.add(a->dx, total * a->channels * e, e, true);
+    sp.add(a->dweight, a->channels * a->taps * we, we, true);
+    sp.add(a->dbias, a->channels * we, we, true);
+    sp.add(a->workspace, need, 16, true);
+    st = sp.check();
+    if (st != FPDE_OK) return st;
+    ConvP P{};
+    P.x = a->x, P.dy = a->dy, P.w = a->weight, P.b = a->bias, P.state = a->state, P.lengths = a->lengths;
+    P.y = a->dx;
+    P.batch = a->batch, P.xb = a->x_batch_stride, P.xt = a->x_time_stride;
+    P.dyb = a->dy_batch_stride, P.dyt = a->dy_time_stride;
+    P.length = (int)a->length, P.channels = (int)a->channels;
+    P.wf32 = a->weight_dtype == FPDE_F32, P.silu = a->silu;
+    P.chunks = cdiv(a->length, kBwdChunk);
+    const int64_t jobs = a->batch * P.chunks;
+    const int64_t n = slots(jobs, a->channels, 16 / e, kBwdWaves), cols = a->channels * a->taps;
+    P.dw = (float*)a->workspace;
+    P.db = a->dbias ? P.dw + n * cols : nullptr;
+    hipStream_t s = (hipStream_t)stream;
+    if (jobs > 0) {
+        st = with_taps(a->dtype, a->taps, [&](auto t, auto w) {
+            using T = decltype(t);
+            return launch(conv_bwd_kernel<T, decltype(w)::value>,
+                          dim3((unsigned)cdiv(a->channels, 64 * kVec<T>), (unsigned)n), dim3(64), s, P);
+        });
+        if (st != FPDE_OK) return st;
+    }
+    const int64_t rows = jobs > 0 ? n : 0;
+    st = queue_colsum(P.dw, rows, cols, cols, a->dweight, a->weight_dtype, s);
+    if (st == FPDE_OK && P.db)
+        st = queue_colsum(P.db, rows, a->channels, a->channels, a->dbias, a->weight_dtype, s);
+    return st;
+}

@@ -1,0 +1,267 @@
+// net_common.hpp -- what the network operators' sources share: element types and
+// their vector loads and stores, wavefront sums, launches and host-side checks.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "fpde_net.h"
+
+namespace fpde_net {
+
+typedef __bf16 bf16;
+typedef _Float16 f16;
+
+// ---------------------------------------------------------------------------
+// Vectors of V elements of type T.  Their declared alignment is the element's:
+// rows of odd widths and sliced tensors are read with the same 16-byte loads
+// (gfx950 takes global accesses of any alignment; a misaligned one costs at most
+// the second cache line that it touches).
+
+template <class T, int V>
+struct Pack {
+    typedef T type __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+};
+template <class T>
+struct Pack<T, 1> {
+    typedef T type;
+};
+
+// elements in 16 bytes
+template <class T>
+constexpr int kVec = 16 / (int)sizeof(T);
+
+template <class T>
+__device__ __forceinline__ float to_f32(T v) {
+    return (float)v;
+}
+// (rounds to nearest, ties to even)
+template <class T>
+__device__ __forceinline__ T from_f32(float v) {
+    return (T)v;
+}
+
+// V elements from p, of which the first n (> 0) exist; the others read as 0
+template <class T, int V>
+__device__ __forceinline__ void load_f32(float (&v)[V], const T* p, int n) {
+    if (n >= V) {
+        const typename Pack<T, V>::type q = *(const typename Pack<T, V>::type*)p;
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = to_f32<T>(q[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = i < n ? to_f32<T>(p[i]) : 0.f;
+    }
+}
+
+template <class T, int V>
+__device__ __forceinline__ void store_f32(T* p, const float (&v)[V], int n) {
+    if (n >= V) {
+        typename Pack<T, V>::type q;
+#pragma unroll
+        for (int i = 0; i < V; ++i) q[i] = from_f32<T>(v[i]);
+        *(typename Pack<T, V>::type*)p = q;
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < n) p[i] = from_f32<T>(v[i]);
+    }
+}
+
+// a parameter array (float32 or the data's type) read as float32
+template <class T, int V>
+__device__ __forceinline__ void load_param(float (&v)[V], const void* p, bool f32, int64_t at,
+                                           int n) {
+    if (f32)
+        load_f32<float, V>(v, (const float*)p + at, n);
+    else
+        load_f32<T, V>(v, (const T*)p + at, n);
+}
+
+template <class T>
+__device__ __forceinline__ float param(const void* p, bool f32, int64_t at) {
+    return f32 ? ((const float*)p)[at] : to_f32<T>(((const T*)p)[at]);
+}
+
+// ---------------------------------------------------------------------------
+// Cross-lane sums and maxima over groups of LANES (a power of two, at most 64)
+// neighbouring lanes; every lane gets the result.
+
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+    return __builtin_bit_cast(
+        float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, false));
+}
+
+struct AddOp {
+    __device__ static float f(float a, float b) { return a + b; }
+};
+struct MaxOp {  // (a NaN loses against a number)
+    __device__ static float f(float a, float b) { return fmaxf(a, b); }
+};
+
+template <int LANES, class Op>
+__device__ __forceinline__ float lanes_reduce(float v) {
+    if (LANES >= 2) v = Op::f(v, dpp<0xB1>(v));   // quad_perm [1,0,3,2]
+    if (LANES >= 4) v = Op::f(v, dpp<0x4E>(v));   // quad_perm [2,3,0,1]
+    if (LANES >= 8) v = Op::f(v, dpp<0x141>(v));  // row_half_mirror
+    if (LANES >= 16) v = Op::f(v, dpp<0x140>(v)); // row_mirror
+    if (LANES >= 32) v = Op::f(v, __shfl_xor(v, 16, 64));
+    if (LANES >= 64) v = Op::f(v, __shfl_xor(v, 32, 64));
+    return v;
+}
+
+// The same over a workgroup of WAVES wavefronts (LANES = 64 * WAVES); red holds
+// WAVES floats of LDS.  Every thread calls it; the barriers are its own.
+template <int LANES, class Op>
+__device__ __forceinline__ float group_reduce(float v, float* red) {
+    v = lanes_reduce<(LANES < 64 ? LANES : 64), Op>(v);
+    if (LANES > 64) {
+        constexpr int W = LANES / 64;
+        __syncthreads();  // (red may still be read from the reduction before)
+        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = red[0];
+#pragma unroll
+        for (int w = 1; w < W; ++w) v = Op::f(v, red[w]);
+    }
+    return v;
+}
+
+// ---------------------------------------------------------------------------
+// Activations, in float32.  exp2 and the reciprocal are the hardware's (1 ulp).
+
+constexpr float kLog2e = 1.44269504088896340736f;
+
+__device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+
+__device__ __forceinline__ float sigmoid(float x) {
+    return __builtin_amdgcn_rcpf(1.f + fast_exp(-x));
+}
+__device__ __forceinline__ float silu(float x) { return x * sigmoid(x); }
+
+// ---------------------------------------------------------------------------
+// Column sums of P partial rows of C floats each, in the order of the rows:
+// the second stage of every sum over rows, time levels or sequences.  A
+// workgroup owns 64 columns; its 16 wavefronts take every 16th row.
+template <class O>
+__global__ __launch_bounds__(1024) void colsum_kernel(const float* __restrict__ part, int64_t rows,
+                                                      int64_t cols, int64_t stride,
+                                                      O* __restrict__ out) {
+    __shared__ float red[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+    float s = 0.f;
+    if (c < cols) {
+        const float* p = part + c;
+        int64_t r = wave;
+        float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+        for (; r + 48 < rows; r += 64) {
+            s0 += p[r * stride];
+            s1 += p[(r + 16) * stride];
+            s2 += p[(r + 32) * stride];
+            s3 += p[(r + 48) * stride];
+        }
+        for (; r < rows; r += 16) s0 += p[r * stride];
+        s = (s0 + s1) + (s2 + s3);
+    }
+    red[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && c < cols) {
+#pragma unroll
+        for (int w = 1; w < 16; ++w) s += red[w][lane];
+        out[c] = from_f32<O>(s);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Host side.
+
+template <class T>
+struct ident {
+    typedef T type;
+};
+
+// Queues k and returns the status of that launch alone.
+template <class... P>
+inline int launch(void (*k)(P...), dim3 grid, dim3 block, hipStream_t s,
+                  typename ident<P>::type... args) {
+    void* a[] = {(void*)&args...};
+    return hipLaunchKernel(reinterpret_cast<const void*>(k), grid, block, a, 0, s) == hipSuccess
+               ? FPDE_OK
+               : FPDE_ERR_HIP;
+}
+
+inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+inline int size_of(int dtype) {
+    return dtype == FPDE_F32 ? 4 : dtype == FPDE_BF16 || dtype == FPDE_F16 ? 2 : 0;
+}
+
+inline int queue_colsum(const float* part, int64_t rows, int64_t cols, int64_t stride, void* out,
+                        int dtype, hipStream_t s) {
+    const dim3 g((unsigned)cdiv(cols, 64)), b(1024);
+    if (dtype == FPDE_F32)
+        return launch(colsum_kernel<float>, g, b, s, part, rows, cols, stride, (float*)out);
+    if (dtype == FPDE_BF16)
+        return launch(colsum_kernel<bf16>, g, b, s, part, rows, cols, stride, (bf16*)out);
+    return launch(colsum_kernel<f16>, g, b, s, part, rows, cols, stride, (f16*)out);
+}
+
+// f(T{}) for the element type of a dtype code that has been checked
+template <class F>
+inline int with_type(int dtype, F f) {
+    switch (dtype) {
+    case FPDE_F32: return f(float{});
+    case FPDE_BF16: return f(bf16{});
+    default: return f(f16{});
+    }
+}
+
+// Buffers of one call: no output may share a byte with another buffer, but for
+// the pairs that a call allows (the same array updated in place).
+struct Span {
+    const char* p;
+    int64_t n;
+    bool out;
+};
+
+struct Spans {
+    Span s[24];
+    int n = 0;
+    int status = FPDE_OK;
+    // p: a buffer of `bytes`, aligned to its element; a NULL one is skipped
+    void add(const void* p, int64_t bytes, int align, bool out) {
+        if (!p || bytes <= 0) return;
+        if ((uintptr_t)p % (unsigned)align) {
+            if (status == FPDE_OK) status = FPDE_ERR_ALIGN;
+            return;
+        }
+        s[n++] = Span{(const char*)p, bytes, out};
+    }
+    int check(const void* pair_a = nullptr, const void* pair_b = nullptr) const {
+        if (status != FPDE_OK) return status;
+        for (int i = 0; i < n; ++i)
+            for (int j = i + 1; j < n; ++j) {
+                if (!s[i].out && !s[j].out) continue;
+                if (s[i].p < s[j].p + s[j].n && s[j].p < s[i].p + s[i].n) {
+                    const bool pair = pair_a && pair_a == pair_b && s[i].p == s[j].p &&
+                                      s[i].n == s[j].n && s[i].p == (const char*)pair_a;
+                    if (!pair) return FPDE_ERR_ARG;
+                }
+            }
+        return FPDE_OK;
+    }
+};
+
+// bytes from the first to the last element of a [n0][n1][n2] array with strides
+// (s0, s1, 1) in elements
+inline int64_t span3(int64_t n0, int64_t n1, int64_t n2, int64_t s0, int64_t s1, int size) {
+    if (n0 <= 0 || n1 <= 0 || n2 <= 0) return 0;
+    return ((n0 - 1) * s0 + (n1 - 1) * s1 + n2) * size;
+}
+
+}  // namespace fpde_net

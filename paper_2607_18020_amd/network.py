@@ -1,0 +1,377 @@
+"""Operators of a time-marching network whose output fields the residual
+operators judge (ctypes binding of libfpde_net, include/fpde_net.h).
+
+A network that marches in time is trained on windows of time levels and then
+answers one level at a time; its fields go into ``binding.ResidualLoss`` or
+``binding.Residual``.  Here are the parts between its weights and its fields:
+
+- ``fpde_rms_norm`` / ``RmsNorm``: root-mean-square norm with the residual
+  stream's addition, with an 8-bit output for answering;
+- ``fpde_causal_conv`` / ``CausalConv``: short causal convolution along time,
+  ``fpde_causal_conv_step`` one level of it;
+- ``fpde_selective_scan`` / ``SelectiveScan``: selective state space scan along
+  time, ``fpde_selective_step`` one level of it;
+- ``fpde_orthogonalize``, ``fpde_muon_step`` / ``Muon``: Newton-Schulz
+  orthogonalised weight updates.
+
+The functions with a C name queue the library's kernels on the current stream
+(or ``stream``) and return tensors; the classes wrap them for autograd and
+optimisers.  As in ``binding``, this module marshals arguments only: there is no
+fallback, and importing a call without the built library fails loudly.  Data
+tensors are float32, bfloat16 or float16 CUDA tensors on the current device.
+"""
+from __future__ import annotations
+
+import ctypes
+import os
+from collections import namedtuple
+from typing import Optional
+
+import torch
+
+from . import binding
+from .binding import FPDE_OK, FpdeError, _stream, _used_on
+
+_HERE = os.path.dirname(os.path.abspath(__file__))
+LIB_PATH = os.path.join(_HERE, "libfpde_net.so")
+
+_CODES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_F8 = 3
+
+_i32, _i64, _f64, _vp = ctypes.c_int32, ctypes.c_int64, ctypes.c_double, ctypes.c_void_p
+
+
+def _fields(spec):
+    """'i32 a b; i64 c; ptr d' -> the _fields_ of a ctypes.Structure."""
+    types = {"i32": _i32, "i64": _i64, "f64": _f64, "ptr": _vp}
+    return [(name, types[part.split()[0]]) for part in spec.split(";") for name in part.split()[1:]]
+
+
+class NormArgs(ctypes.Structure):
+    _fields_ = _fields("i32 dtype weight_dtype out_dtype group; i64 rows width x_stride residual_stride; "
+                       "f64 eps; ptr x residual weight y sum scales")
+
+
+class NormBwdArgs(ctypes.Structure):
+    _fields_ = _fields("i32 dtype weight_dtype; i64 rows width dy_stride sum_stride dsum_stride; f64 eps; "
+                       "ptr dy sum dsum weight ds dweight workspace; i64 workspace_bytes")
+
+
+class ConvArgs(ctypes.Structure):
+    _fields_ = _fields("i32 dtype weight_dtype taps silu; i64 batch length channels x_batch_stride x_time_stride; "
+                       "ptr x weight bias state lengths y state_out")
+
+
+class ConvBwdArgs(ctypes.Structure):
+    _fields_ = _fields("i32 dtype weight_dtype taps silu; i64 batch length channels x_batch_stride x_time_stride "
+                       "dy_batch_stride dy_time_stride; ptr dy x weight bias state lengths dx dweight dbias "
+                       "workspace; i64 workspace_bytes")
+
+
+# entry points and their argument structs; those with a workspace also have a
+# function ending in _workspace
+CALLS = {"fpde_rms_norm": (NormArgs, False), "fpde_rms_norm_bwd": (NormBwdArgs, True),
+         "fpde_causal_conv": (ConvArgs, False), "fpde_causal_conv_bwd": (ConvBwdArgs, True)}
+EXPORTED = tuple(CALLS) + tuple(n + "_workspace" for n, (_, ws) in CALLS.items() if ws)
+
+_lib = None
+
+
+def _load():
+    global _lib
+    if _lib is None:
+        if not os.path.exists(LIB_PATH):
+            raise ImportError(f"{LIB_PATH} is not built; run `python -m paper_2607_18020_amd.csrc.build`")
+        lib_ = ctypes.CDLL(LIB_PATH)
+        for name, (args, ws) in CALLS.items():
+            fn = getattr(lib_, name)
+            fn.argtypes, fn.restype = [ctypes.POINTER(args), _vp], ctypes.c_int
+            if ws:
+                fn = getattr(lib_, name + "_workspace")
+                fn.argtypes, fn.restype = [ctypes.POINTER(args)], _i64
+        _lib = lib_
+    return _lib
+
+
+def lib():
+    """The loaded ctypes library (raises ImportError if it is not built)."""
+    return _load()
+
+
+def _call(name, args, stream):
+    st = getattr(_lib or _load(), name)(args, _stream(stream))
+    if st != FPDE_OK:
+        raise FpdeError(st, name)
+
+
+def _workspace(name, args, dev, stream):
+    """Allocates what the call needs and enters it in ``args``."""
+    n = getattr(_lib or _load(), name + "_workspace")(args)
+    if n < 0:
+        raise FpdeError(n, name)
+    if n:
+        ws = torch.empty(n, dtype=torch.uint8, device=dev)
+        if stream is not None:
+            _used_on(stream, ws)
+        args.workspace, args.workspace_bytes = ws.data_ptr(), n
+
+
+# ---------------------------------------------------------------------------
+# Checks.  Sizes, strides and overlaps are checked by the C side too; here is
+# what only the tensors know: devices, types, and shapes that have to agree.
+
+def _data(what, t, dev=None, dtype=None):
+    """A data tensor's type code; on the current device, or on ``dev``."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{what}: need a CUDA tensor")
+    code = _CODES.get(t.dtype)
+    if code is None or (dtype is not None and t.dtype is not dtype):
+        raise ValueError(f"{what}: dtype {t.dtype}, need " +
+                         (str(dtype) if dtype is not None else "float32, bfloat16 or float16"))
+    if dev is None:
+        if t.device.index != torch.cuda.current_device():
+            raise ValueError(f"{what}: tensor on {t.device}, current device is "
+                             f"cuda:{torch.cuda.current_device()}")
+    elif t.device != dev:
+        raise ValueError(f"{what}: tensors on different devices ({dev}, {t.device})")
+    return code
+
+
+def _dense(what, t, shape, dtype, dev):
+    """A dense tensor of this shape, type and device."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.shape != shape or t.device != dev \
+            or not t.is_contiguous():
+        raise ValueError(f"{what}: need a contiguous {dtype} tensor of shape {tuple(shape)} on {dev}")
+    return t.data_ptr()
+
+
+def _param(what, t, shape, dtype, dev):
+    """A dense parameter in float32 or the data's type."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in (torch.float32, dtype):
+        raise ValueError(f"{what}: need a float32 or {dtype} tensor")
+    return _dense(what, t, shape, t.dtype, dev)
+
+
+def _rows(what, t):
+    """(rows, width, row stride) of a tensor whose leading axes fold into one."""
+    n = t.dim()
+    if n == 0 or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{what}: the last axis has to be dense")
+    width = t.shape[-1]
+    if t.is_contiguous():
+        return (t.numel() // width if width else 0), width, width
+    rows, stride = 1, width
+    for a in range(n - 2, -1, -1):
+        if t.shape[a] == 1:
+            continue
+        if rows == 1:
+            stride = t.stride(a)
+        elif t.stride(a) != stride * rows:
+            raise ValueError(f"{what}: leading axes with strides {t.stride()} do not fold into rows")
+        rows *= t.shape[a]
+    if rows > 1 and stride < width:
+        raise ValueError(f"{what}: rows with strides {t.stride()} overlap")
+    return rows, width, max(stride, width)
+
+
+def _levels(what, t):
+    """(batch, length, channels, batch stride, time stride) of a [B, L, D] tensor."""
+    if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError(f"{what}: need [batch, length, channels] with dense channels")
+    return (*t.shape, t.stride(0), t.stride(1))
+
+
+def _empty(stream, shape, dtype, dev):
+    t = torch.empty(shape, dtype=dtype, device=dev)
+    if stream is not None:
+        _used_on(stream, t)
+    return t
+
+
+# ---------------------------------------------------------------------------
+# Root-mean-square norm.
+
+def fpde_rms_norm(x, weight=None, *, residual=None, eps: float = 1e-6, quant: Optional[int] = None, out=None,
+                  sum_out=None, stream=None):
+    """Queue s = x + residual, y = weight * s / sqrt(mean(s^2) + eps) over the last
+    axis.  Returns (y, s), with s = x itself where there is no residual.
+
+    ``quant``: 128 (columns) or 0 (a whole row): y in 8 bits (float8_e4m3fn) with one
+    float32 scale per group; returns (q, scales, s), y being about q * scale.
+    ``out`` / ``sum_out``: dense tensors to write y (or q) and s to; ``sum_out`` may be
+    a dense x or residual.  Leading axes of any strides that fold into rows."""
+    code = _data("fpde_rms_norm x", x)
+    dev, dt = x.device, x.dtype
+    rows, width, xs = _rows("fpde_rms_norm x", x)
+    rp = rs = sp = None
+    if residual is not None:
+        _data("fpde_rms_norm residual", residual, dev, dt)
+        if residual.shape != x.shape:
+            raise ValueError(f"fpde_rms_norm: residual {tuple(residual.shape)} is not like x {tuple(x.shape)}")
+        rs, rp = _rows("fpde_rms_norm residual", residual)[2], residual.data_ptr()
+    if sum_out is not None:
+        sp = _dense("fpde_rms_norm sum_out", sum_out, x.shape, dt, dev)
+    elif residual is not None:
+        sum_out = _empty(stream, x.shape, dt, dev)
+        sp = sum_out.data_ptr()
+    wp, wcode = None, code
+    if weight is not None:
+        wp, wcode = _param("fpde_rms_norm weight", weight, (width,), dt, dev), _CODES[weight.dtype]
+    scales = None
+    odt = dt if quant is None else torch.float8_e4m3fn
+    if out is None:
+        out = _empty(stream, x.shape, odt, dev)
+    else:
+        _dense("fpde_rms_norm out", out, x.shape, odt, dev)
+    if quant is not None:
+        groups = 1 if quant == 0 else -(-width // quant)
+        scales = _empty(stream, (*x.shape[:-1], groups), torch.float32, dev)
+    a = NormArgs(code, wcode, code if quant is None else _F8, quant or 0, rows, width, xs, rs or 0, eps,
+                 x.data_ptr(), rp, wp, out.data_ptr(), sp, None if scales is None else scales.data_ptr())
+    _call("fpde_rms_norm", a, stream)
+    s = x if sum_out is None else sum_out
+    return (out, s) if quant is None else (out, scales, s)
+
+
+def fpde_rms_norm_bwd(dy, s, weight=None, *, dsum=None, eps: float = 1e-6, want_dweight: bool = True, ds=None,
+                      stream=None):
+    """Queue the gradients of ``fpde_rms_norm``: returns (ds, dweight).  ``s`` is what
+    the forward returned, ``dsum`` the gradient that reaches it by the residual
+    stream; ds is the gradient of x and of the residual alike.  ``ds`` may be a
+    dense dy or dsum, updated in place.  dweight is None without a weight."""
+    code = _data("fpde_rms_norm_bwd dy", dy)
+    dev, dt = dy.device, dy.dtype
+    _data("fpde_rms_norm_bwd s", s, dev, dt)
+    if s.shape != dy.shape:
+        raise ValueError(f"fpde_rms_norm_bwd: s {tuple(s.shape)} is not like dy {tuple(dy.shape)}")
+    rows, width, dys = _rows("fpde_rms_norm_bwd dy", dy)
+    ss = _rows("fpde_rms_norm_bwd s", s)[2]
+    dp, dss = None, 0
+    if dsum is not None:
+        _data("fpde_rms_norm_bwd dsum", dsum, dev, dt)
+        if dsum.shape != dy.shape:
+            raise ValueError(f"fpde_rms_norm_bwd: dsum {tuple(dsum.shape)} is not like dy {tuple(dy.shape)}")
+        dss, dp = _rows("fpde_rms_norm_bwd dsum", dsum)[2], dsum.data_ptr()
+    wp, wcode, dweight = None, code, None
+    if weight is not None:
+        wp, wcode = _param("fpde_rms_norm_bwd weight", weight, (width,), dt, dev), _CODES[weight.dtype]
+        if want_dweight:
+            dweight = _empty(stream, (width,), weight.dtype, dev)
+    if ds is None:
+        ds = _empty(stream, dy.shape, dt, dev)
+    else:
+        _dense("fpde_rms_norm_bwd ds", ds, dy.shape, dt, dev)
+    a = NormBwdArgs(code, wcode, rows, width, dys, ss, dss, eps, dy.data_ptr(), s.data_ptr(), dp, wp,
+                    ds.data_ptr(), None if dweight is None else dweight.data_ptr(), None, 0)
+    _workspace("fpde_rms_norm_bwd", a, dev, stream)
+    _call("fpde_rms_norm_bwd", a, stream)
+    return ds, dweight
+
+
+class RmsNorm(torch.autograd.Function):
+    """``y, s = RmsNorm.apply(x, residual, weight, eps)``: the norm of the residual
+    stream s = x + residual (residual and weight may be None)."""
+
+    @staticmethod
+    def forward(ctx, x, residual, weight, eps=1e-6):
+        y, s = fpde_rms_norm(x, weight, residual=residual, eps=eps)
+        ctx.eps, ctx.with_residual = eps, residual is not None
+        ctx.save_for_backward(s, weight)
+        return y, (s if residual is not None else s.view_as(s))
+
+    @staticmethod
+    def backward(ctx, dy, dsum):
+        s, weight = ctx.saved_tensors
+        dy = torch.zeros_like(s) if dy is None else dy.to(s.dtype).contiguous()
+        dsum = None if dsum is None else dsum.to(s.dtype).contiguous()
+        ds, dw = fpde_rms_norm_bwd(dy, s, weight, dsum=dsum, eps=ctx.eps, want_dweight=ctx.needs_input_grad[2])
+        return ds, (ds if ctx.with_residual else None), dw, None
+
+
+# ---------------------------------------------------------------------------
+# Short causal convolution along time.
+
+def _conv_common(what, x, weight, bias, state, lengths):
+    code = _data(f"{what} x", x)
+    dev, dt = x.device, x.dtype
+    B, L, D, bs, ts = _levels(f"{what} x", x)
+    if not isinstance(weight, torch.Tensor) or weight.dim() != 2:
+        raise ValueError(f"{what} weight: need [channels, taps]")
+    W = weight.shape[1]
+    wp = _param(f"{what} weight", weight, (D, W), dt, dev)
+    bp = None if bias is None else _dense(f"{what} bias", bias, (D,), weight.dtype, dev)
+    sp = None if state is None else _dense(f"{what} state", state, (B, W - 1, D), dt, dev)
+    lp = None if lengths is None else _dense(f"{what} lengths", lengths, (B,), torch.int32, dev)
+    return code, B, L, D, bs, ts, W, wp, bp, sp, lp
+
+
+def fpde_causal_conv(x, weight, bias=None, *, silu: bool = True, state=None, lengths=None, state_out=None, out=None,
+                     stream=None):
+    """Queue the causal convolution of x [B, L, D] along its levels with weight [D,
+    taps] (2 to 4 taps, the last on the present level), bias and silu.  ``state``
+    [B, taps - 1, D]: the levels before the window (zero without); ``state_out``: gets
+    the last ones (may be ``state``).  ``lengths`` (int32 [B]): levels of each
+    sequence; y is zero past them.  Returns y."""
+    what = "fpde_causal_conv"
+    code, B, L, D, bs, ts, W, wp, bp, sp, lp = _conv_common(what, x, weight, bias, state, lengths)
+    dev, dt = x.device, x.dtype
+    so = None if state_out is None else _dense(f"{what} state_out", state_out, (B, W - 1, D), dt, dev)
+    if out is None:
+        out = _empty(stream, (B, L, D), dt, dev)
+    else:
+        _dense(f"{what} out", out, (B, L, D), dt, dev)
+    _call(what, ConvArgs(code, _CODES[weight.dtype], W, bool(silu), B, L, D, bs, ts, x.data_ptr(), wp, bp, sp, lp,
+                         out.data_ptr(), so), stream)
+    return out
+
+
+def fpde_causal_conv_step(x, state, weight, bias=None, *, silu: bool = True, out=None, stream=None):
+    """One level of ``fpde_causal_conv``: x [B, D]; ``state`` [B, taps - 1, D] is read
+    and updated in place.  Returns y [B, D]."""
+    if not isinstance(x, torch.Tensor) or x.dim() != 2:
+        raise ValueError("fpde_causal_conv_step x: need [batch, channels]")
+    if state is None:
+        raise ValueError("fpde_causal_conv_step: needs a state")
+    y = fpde_causal_conv(x.unsqueeze(1), weight, bias, silu=silu, state=state, state_out=state,
+                         out=None if out is None else out.unsqueeze(1), stream=stream)
+    return y.squeeze(1)
+
+
+def fpde_causal_conv_bwd(dy, x, weight, bias=None, *, silu: bool = True, state=None, lengths=None, stream=None):
+    """Queue the gradients of ``fpde_causal_conv``: returns (dx, dweight, dbias), dbias
+    None without a bias.  The carried state is data: no gradient goes through it."""
+    what = "fpde_causal_conv_bwd"
+    code, B, L, D, bs, ts, W, wp, bp, sp, lp = _conv_common(what, x, weight, bias, state, lengths)
+    dev, dt = x.device, x.dtype
+    _data(f"{what} dy", dy, dev, dt)
+    if dy.shape != x.shape:
+        raise ValueError(f"{what}: dy {tuple(dy.shape)} is not like x {tuple(x.shape)}")
+    _, _, _, dbs, dts = _levels(f"{what} dy", dy)
+    dx = _empty(stream, (B, L, D), dt, dev)
+    dw = _empty(stream, (D, W), weight.dtype, dev)
+    db = None if bias is None else _empty(stream, (D,), weight.dtype, dev)
+    a = ConvBwdArgs(code, _CODES[weight.dtype], W, bool(silu), B, L, D, bs, ts, dbs, dts, dy.data_ptr(),
+                    x.data_ptr(), wp, bp, sp, lp, dx.data_ptr(), dw.data_ptr(), None if db is None else db.data_ptr(),
+                    None, 0)
+    _workspace(what, a, dev, stream)
+    _call(what, a, stream)
+    return dx, dw, db
+
+
+class CausalConv(torch.autograd.Function):
+    """``y = CausalConv.apply(x, weight, bias, silu, state, lengths)``."""
+
+    @staticmethod
+    def forward(ctx, x, weight, bias=None, silu=True, state=None, lengths=None):
+        if state is not None and state.requires_grad:
+            raise ValueError("CausalConv: no gradient goes through the carried state; detach it")
+        ctx.silu = silu
+        ctx.save_for_backward(x, weight, bias, state, lengths)
+        return fpde_causal_conv(x, weight, bias, silu=silu, state=state, lengths=lengths)
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, weight, bias, state, lengths = ctx.saved_tensors
+        dx, dw, db = fpde_causal_conv_bwd(dy.contiguous(), x, weight, bias, silu=ctx.silu, state=state,
+                                          lengths=lengths)
+        return dx, dw, db, None, None, None
