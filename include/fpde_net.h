@@ -169,6 +169,91 @@ typedef struct fpde_conv_bwd_args {
 int64_t fpde_causal_conv_bwd_workspace(const fpde_conv_bwd_args* a); /* (reads sizes and types) */
 int fpde_causal_conv_bwd(const fpde_conv_bwd_args* a, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Selective state space scan along time.  Channel c of sequence b carries
+ * `states` states h[n]; group c / (channels / groups) gives it B and C:
+ *     d = delta[b][t][c] + delta_bias[c],   dt = softplus(d) (or d itself)
+ *     h[n] = exp(dt * A[c][n]) * h[n] + dt * B[b][t][g][n] * u[b][t][c]
+ *     y    = sum_n C[b][t][g][n] * h[n] + D[c] * u[b][t][c]
+ *     out  = y, or y * z * sigmoid(z) with z.
+ * h starts from state[b][c][n], or from zero.  Sequence b holds lengths[b] levels
+ * (NULL: `length`; clamped to 0 .. length): out is 0 past them, nothing is read
+ * there, and state_out gets h after the last of them.  A single level (length 1)
+ * with state_out = state is the step of a rollout.  A, D, delta_bias and states
+ * are float32 whatever the data's type.
+ *
+ * Limits: 1 <= states <= 32 (FPDE_ERR_UNSUPPORTED above), groups divides channels,
+ * 1 <= channels <= 2^20, 0 <= batch, 0 <= length < 2^31 - 256,
+ * batch * length <= 2^40. */
+typedef struct fpde_scan_args {
+    int32_t dtype;            /* u, delta, B, C, z, y */
+    int32_t states, groups;
+    int32_t softplus;         /* 0 or 1 */
+    int64_t batch, length, channels;
+    int64_t u_batch_stride, u_time_stride;
+    int64_t delta_batch_stride, delta_time_stride;
+    int64_t z_batch_stride, z_time_stride;
+    int64_t b_batch_stride, b_time_stride;   /* of [batch][length][groups][states] */
+    int64_t c_batch_stride, c_time_stride;
+    const void* u;
+    const void* delta;
+    const float* A;           /* [channels][states] */
+    const void* B;
+    const void* C;
+    const float* D;           /* [channels] or NULL: zero */
+    const void* z;            /* or NULL: no gate */
+    const float* delta_bias;  /* [channels] or NULL: zero */
+    const float* state;       /* [batch][channels][states] or NULL */
+    const int32_t* lengths;   /* [batch] or NULL */
+    void* y;                  /* [batch][length][channels] */
+    float* state_out;         /* [batch][channels][states] or NULL; may be `state` */
+    void* workspace;
+    int64_t workspace_bytes;
+} fpde_scan_args;
+
+int64_t fpde_selective_scan_workspace(const fpde_scan_args* a); /* (reads sizes and types) */
+int fpde_selective_scan(const fpde_scan_args* a, void* stream);
+
+/* Gradients of fpde_selective_scan for dy, the gradient of `out`; the carried
+ * state is data (no gradient goes through it).  Gradients of data are 0 past a
+ * sequence's levels, where dy is not read. */
+typedef struct fpde_scan_bwd_args {
+    int32_t dtype;
+    int32_t states, groups;
+    int32_t softplus;
+    int64_t batch, length, channels;
+    int64_t u_batch_stride, u_time_stride;
+    int64_t delta_batch_stride, delta_time_stride;
+    int64_t z_batch_stride, z_time_stride;
+    int64_t b_batch_stride, b_time_stride;
+    int64_t c_batch_stride, c_time_stride;
+    int64_t dy_batch_stride, dy_time_stride;
+    const void* u;
+    const void* delta;
+    const float* A;
+    const void* B;
+    const void* C;
+    const float* D;
+    const void* z;
+    const float* delta_bias;
+    const float* state;
+    const int32_t* lengths;
+    const void* dy;
+    void* du;                 /* [batch][length][channels], as ddelta and dz */
+    void* ddelta;
+    float* dA;                /* [channels][states] */
+    void* dB;                 /* [batch][length][groups][states], as dC */
+    void* dC;
+    float* dD;                /* [channels]; NULL if and only if D is */
+    void* dz;                 /* NULL if and only if z is */
+    float* ddelta_bias;       /* [channels]; NULL if and only if delta_bias is */
+    void* workspace;
+    int64_t workspace_bytes;
+} fpde_scan_bwd_args;
+
+int64_t fpde_selective_scan_bwd_workspace(const fpde_scan_bwd_args* a); /* (reads sizes and types) */
+int fpde_selective_scan_bwd(const fpde_scan_bwd_args* a, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -68,10 +68,26 @@ class ConvBwdArgs(ctypes.Structure):
                        "workspace; i64 workspace_bytes")
 
 
+_SCAN_HEAD = ("i32 dtype states groups softplus; i64 batch length channels u_batch_stride u_time_stride "
+              "delta_batch_stride delta_time_stride z_batch_stride z_time_stride b_batch_stride b_time_stride "
+              "c_batch_stride c_time_stride")
+_SCAN_IN = "ptr u delta A B C D z delta_bias state lengths"
+
+
+class ScanArgs(ctypes.Structure):
+    _fields_ = _fields(f"{_SCAN_HEAD}; {_SCAN_IN} y state_out workspace; i64 workspace_bytes")
+
+
+class ScanBwdArgs(ctypes.Structure):
+    _fields_ = _fields(f"{_SCAN_HEAD} dy_batch_stride dy_time_stride; {_SCAN_IN} dy du ddelta dA dB dC dD dz "
+                       "ddelta_bias workspace; i64 workspace_bytes")
+
+
 # entry points and their argument structs; those with a workspace also have a
 # function ending in _workspace
 CALLS = {"fpde_rms_norm": (NormArgs, False), "fpde_rms_norm_bwd": (NormBwdArgs, True),
-         "fpde_causal_conv": (ConvArgs, False), "fpde_causal_conv_bwd": (ConvBwdArgs, True)}
+         "fpde_causal_conv": (ConvArgs, False), "fpde_causal_conv_bwd": (ConvBwdArgs, True),
+         "fpde_selective_scan": (ScanArgs, True), "fpde_selective_scan_bwd": (ScanBwdArgs, True)}
 EXPORTED = tuple(CALLS) + tuple(n + "_workspace" for n, (_, ws) in CALLS.items() if ws)
 
 _lib = None
@@ -375,3 +391,127 @@ class CausalConv(torch.autograd.Function):
         dx, dw, db = fpde_causal_conv_bwd(dy.contiguous(), x, weight, bias, silu=ctx.silu, state=state,
                                           lengths=lengths)
         return dx, dw, db, None, None, None
+
+
+# ---------------------------------------------------------------------------
+# Selective state space scan along time.
+
+def _scan_common(what, u, delta, A, B, C, D, z, delta_bias, softplus, state, lengths):
+    """The arguments that both directions share: (head, inputs, dims)."""
+    code = _data(f"{what} u", u)
+    dev, dt = u.device, u.dtype
+    Bn, L, Dn, ubs, uts = _levels(f"{what} u", u)
+    if not isinstance(A, torch.Tensor) or A.dim() != 2:
+        raise ValueError(f"{what} A: need [channels, states]")
+    n = A.shape[1]
+    strides = [ubs, uts]
+    for name, t in (("delta", delta), ("z", z)):
+        if t is None:
+            strides += [0, 0]
+            continue
+        _data(f"{what} {name}", t, dev, dt)
+        if t.shape != u.shape:
+            raise ValueError(f"{what}: {name} {tuple(t.shape)} is not like u {tuple(u.shape)}")
+        strides += _levels(f"{what} {name}", t)[3:]
+    groups = B.shape[2] if isinstance(B, torch.Tensor) and B.dim() == 4 else 1
+    for name, t in (("B", B), ("C", C)):
+        _data(f"{what} {name}", t, dev, dt)
+        if t.shape != (Bn, L, groups, n) and (groups > 1 or t.shape != (Bn, L, n)):
+            raise ValueError(f"{what} {name}: need [batch, length, groups, states] (or without groups)")
+        if (n > 1 and t.stride(-1) != 1) or (groups > 1 and t.stride(2) != n):
+            raise ValueError(f"{what} {name}: groups and states have to be dense")
+        strides += [t.stride(0), t.stride(1)]
+    f32 = torch.float32
+    ptrs = [u.data_ptr(), delta.data_ptr(), _dense(f"{what} A", A, (Dn, n), f32, dev), B.data_ptr(), C.data_ptr(),
+            None if D is None else _dense(f"{what} D", D, (Dn,), f32, dev), None if z is None else z.data_ptr(),
+            None if delta_bias is None else _dense(f"{what} delta_bias", delta_bias, (Dn,), f32, dev),
+            None if state is None else _dense(f"{what} state", state, (Bn, Dn, n), f32, dev),
+            None if lengths is None else _dense(f"{what} lengths", lengths, (Bn,), torch.int32, dev)]
+    return [code, n, groups, bool(softplus), Bn, L, Dn, *strides], ptrs, (Bn, L, Dn, groups, n)
+
+
+def fpde_selective_scan(u, delta, A, B, C, *, D=None, z=None, delta_bias=None, softplus: bool = True, state=None,
+                        lengths=None, state_out=None, out=None, stream=None):
+    """Queue the selective scan of u [b, L, channels] along its levels:
+
+        dt = softplus(delta + delta_bias);  h = exp(dt A) h + dt B u;
+        y = (sum_n C h + D u) * silu(z)
+
+    A [channels, states] (float32, up to 32 states); B, C [b, L, groups, states] or
+    [b, L, states]; D, delta_bias [channels] float32; ``state`` / ``state_out``
+    [b, channels, states] float32 (the same tensor: updated in place); ``lengths``
+    (int32 [b]): levels of each sequence, y being zero past them.  Returns y."""
+    what = "fpde_selective_scan"
+    head, ptrs, (Bn, L, Dn, _, n) = _scan_common(what, u, delta, A, B, C, D, z, delta_bias, softplus, state, lengths)
+    dev, dt = u.device, u.dtype
+    so = None if state_out is None else _dense(f"{what} state_out", state_out, (Bn, Dn, n), torch.float32, dev)
+    if out is None:
+        out = _empty(stream, (Bn, L, Dn), dt, dev)
+    else:
+        _dense(f"{what} out", out, (Bn, L, Dn), dt, dev)
+    a = ScanArgs(*head, *ptrs, out.data_ptr(), so, None, 0)
+    if L > 1:
+        _workspace(what, a, dev, stream)
+    _call(what, a, stream)
+    return out
+
+
+def fpde_selective_step(state, u, delta, A, B, C, *, D=None, z=None, delta_bias=None, softplus: bool = True,
+                        out=None, stream=None):
+    """One level of ``fpde_selective_scan``: u, delta, z [b, channels], B, C [b, groups,
+    states] or [b, states]; ``state`` [b, channels, states] is read and updated in
+    place.  Returns y [b, channels]."""
+    if state is None or not isinstance(u, torch.Tensor) or u.dim() != 2:
+        raise ValueError("fpde_selective_step: needs a state and u [batch, channels]")
+    one = [None if t is None else t.unsqueeze(1) for t in (u, delta, B, C, z, out)]
+    y = fpde_selective_scan(one[0], one[1], A, one[2], one[3], D=D, z=one[4], delta_bias=delta_bias,
+                            softplus=softplus, state=state, state_out=state, out=one[5], stream=stream)
+    return y.squeeze(1)
+
+
+ScanGrads = namedtuple("ScanGrads", "du ddelta dA dB dC dD dz ddelta_bias")
+
+
+def fpde_selective_scan_bwd(dy, u, delta, A, B, C, *, D=None, z=None, delta_bias=None, softplus: bool = True,
+                            state=None, lengths=None, stream=None) -> ScanGrads:
+    """Queue the gradients of ``fpde_selective_scan`` for dy, the gradient of its
+    output: a ScanGrads (dD, dz, ddelta_bias None where the input is).  The carried
+    state is data: no gradient goes through it."""
+    what = "fpde_selective_scan_bwd"
+    head, ptrs, (Bn, L, Dn, groups, n) = _scan_common(what, u, delta, A, B, C, D, z, delta_bias, softplus, state,
+                                                      lengths)
+    dev, dt = u.device, u.dtype
+    _data(f"{what} dy", dy, dev, dt)
+    if dy.shape != u.shape:
+        raise ValueError(f"{what}: dy {tuple(dy.shape)} is not like u {tuple(u.shape)}")
+    dys = _levels(f"{what} dy", dy)[3:]
+    f32 = torch.float32
+    g = ScanGrads(_empty(stream, (Bn, L, Dn), dt, dev), _empty(stream, (Bn, L, Dn), dt, dev),
+                  _empty(stream, (Dn, n), f32, dev), _empty(stream, B.shape, dt, dev), _empty(stream, C.shape, dt, dev),
+                  None if D is None else _empty(stream, (Dn,), f32, dev),
+                  None if z is None else _empty(stream, (Bn, L, Dn), dt, dev),
+                  None if delta_bias is None else _empty(stream, (Dn,), f32, dev))
+    a = ScanBwdArgs(*head, *dys, *ptrs, dy.data_ptr(), *[None if t is None else t.data_ptr() for t in g], None, 0)
+    _workspace(what, a, dev, stream)
+    _call(what, a, stream)
+    return g
+
+
+class SelectiveScan(torch.autograd.Function):
+    """``y = SelectiveScan.apply(u, delta, A, B, C, D, z, delta_bias, softplus, state, lengths)``."""
+
+    @staticmethod
+    def forward(ctx, u, delta, A, B, C, D=None, z=None, delta_bias=None, softplus=True, state=None, lengths=None):
+        if state is not None and state.requires_grad:
+            raise ValueError("SelectiveScan: no gradient goes through the carried state; detach it")
+        ctx.softplus = softplus
+        ctx.save_for_backward(u, delta, A, B, C, D, z, delta_bias, state, lengths)
+        return fpde_selective_scan(u, delta, A, B, C, D=D, z=z, delta_bias=delta_bias, softplus=softplus, state=state,
+                                   lengths=lengths)
+
+    @staticmethod
+    def backward(ctx, dy):
+        u, delta, A, B, C, D, z, bias, state, lengths = ctx.saved_tensors
+        g = fpde_selective_scan_bwd(dy.contiguous(), u, delta, A, B, C, D=D, z=z, delta_bias=bias,
+                                    softplus=ctx.softplus, state=state, lengths=lengths)
+        return (*g, None, None, None)

@@ -72,3 +72,29 @@ def causal_conv(x, w, b, act, state, lengths):
         y[i, :n] = silu(p) if act else p
         last[i] = e[n:]
     return y, last
+
+
+def softplus(x):
+    return x.clamp(min=0) + torch.log1p(torch.exp(-x.abs()))
+
+
+def selective_scan(u, delta, A, B, C, D, z, bias, sp, state, lengths):
+    """(y, state after the last level) from the definition, level by level.  B, C: [b, L, G, N]."""
+    Bn, L, Dn = u.shape
+    group = torch.arange(Dn) // (Dn // B.shape[2])
+    raw = delta if bias is None else delta + bias
+    dt = softplus(raw) if sp else raw
+    h = torch.zeros(Bn, *A.shape, dtype=u.dtype) if state is None else state
+    n = torch.full((Bn,), L) if lengths is None else lengths.clamp(0, L)
+    ys = []
+    for t in range(L):
+        on = (n > t)[:, None, None]
+        new = torch.exp(dt[:, t, :, None] * A) * h + (dt[:, t] * u[:, t])[..., None] * B[:, t, group]
+        h = torch.where(on, new, h)
+        y = (h * C[:, t, group]).sum(-1)
+        if D is not None:
+            y = y + D * u[:, t]
+        if z is not None:
+            y = y * silu(z[:, t])
+        ys.append(torch.where(on[..., 0], y, torch.zeros((), dtype=y.dtype)))
+    return (torch.stack(ys, 1) if ys else torch.zeros_like(u)), h

@@ -1,0 +1,307 @@
+"""fpde_selective_scan, its single-level step and its gradients against float64:
+every number of states and workgroup width, windows split in chunks, ragged
+lengths (none among them), groups, carried states, strides, streams, graphs.
+
+Tolerances.  The state's chain of multiply-adds contracts (the decays are below 1),
+so that an error made at a level fades as the state does: relative to the sum of
+the magnitudes of what is added (the same scan with |u|, |B|, |C|, |state|) each level
+adds a few roundings, and the decays' own, |dt A| 2^-24 each, add up to (sum of |dt
+A| over the window that the state remembers, at most about 1) + 2 an exponential for
+each level of it.  CHAIN covers the levels that a state with dt A <= -0.02 remembers
+to 10 %, with 8 roundings each.  Gradients pass twice through such chains."""
+from __future__ import annotations
+
+import pytest
+import torch
+
+from tests import network_ref as R
+
+pytestmark = pytest.mark.gpu
+CHAIN = 8 * 128
+NAMES = ("u", "delta", "A", "B", "C", "D", "z", "bias")
+
+
+@pytest.fixture(scope="module")
+def N():
+    from paper_2607_18020_amd import network
+    network.lib()
+    return network
+
+
+def inputs(b, L, D, n, G, dt, seed=0):
+    g = torch.Generator().manual_seed(seed + b * 7919 + L * 31 + D * 3 + n)
+    step = 0.02 + 0.2 * torch.rand(D, generator=g, dtype=torch.float64)
+    t = dict(u=R.randn(g, b, L, D, dtype=dt), delta=(0.5 * R.randn(g, b, L, D)).to(dt),
+             A=-(1 + 3 * torch.rand(D, n, generator=g)), B=R.randn(g, b, L, G, n, dtype=dt),
+             C=R.randn(g, b, L, G, n, dtype=dt), D=R.randn(g, D), z=R.randn(g, b, L, D, dtype=dt),
+             bias=torch.log(torch.expm1(step)).float(), state=R.randn(g, b, D, n), dy=R.randn(g, b, L, D, dtype=dt),
+             lengths=torch.randint(0, L + 1, (b,), generator=g, dtype=torch.int32))
+    t["lengths"][0] = L
+    return t
+
+
+def cuda(t):
+    return {k: v.cuda() for k, v in t.items()}
+
+
+def call(N, c, sp=True, drop=(), **kw):
+    o = {k: None if k in drop else c[v] for k, v in (("D", "D"), ("z", "z"), ("delta_bias", "bias"),
+                                                      ("state", "state"), ("lengths", "lengths"))}
+    o.update(kw)
+    return (c["u"], c["delta"], c["A"], c["B"], c["C"]), dict(o, softplus=sp)
+
+
+def mag_inputs(f):
+    """The same problem with every term's magnitude."""
+    m = dict(f)
+    for k in ("u", "B", "C", "D", "state"):
+        m[k] = f[k].abs()
+    return m
+
+
+def reference(f, sp, drop, grad=True):
+    leaf = {k: f[k].clone().requires_grad_(grad) for k in NAMES}
+    o = {k: None if k in drop else v for k, v in (("D", leaf["D"]), ("z", leaf["z"]), ("delta_bias", leaf["bias"]),
+                                                  ("state", f["state"]), ("lengths", f["lengths"]))}
+    y, h = R.selective_scan(leaf["u"], leaf["delta"], leaf["A"], leaf["B"], leaf["C"], o["D"], o["z"],
+                            o["delta_bias"], sp, o["state"], o["lengths"])
+    return leaf, y, h
+
+
+def f64(t):
+    return {k: v if v.dtype is torch.int32 else v.double() for k, v in t.items()}
+
+
+def check(N, t, sp, drop, what):
+    c, f = cuda(t), f64(t)
+    args, opts = call(N, c, sp, drop)
+    last = torch.full_like(c["state"], float("nan"))
+    y = N.fpde_selective_scan(*args, state_out=last, **opts)
+    leaf, ry, rh = reference(f, sp, drop)
+    # magnitudes: z's gate stays as it is, |silu| <= |z|
+    m = mag_inputs(f)
+    _, my, mh = reference(dict(m, z=f["z"]), sp, set(drop) | {"z"}, grad=False)
+    gate = 1 if "z" in drop else f["z"].abs()
+    R.close(what + " y", y, ry.detach(), CHAIN, my * gate)
+    R.close(what + " state", last, rh.detach(), CHAIN, mh)
+    (ry * f["dy"]).sum().backward()
+    g = N.fpde_selective_scan_bwd(c["dy"], *args, **opts)
+    # the gradients of the problem of magnitudes, decays as they are: what each gradient's terms add up
+    # to.  With a gate its own error is of the order of |z| + 1 of them.
+    k = 1 if "z" in drop else (f["z"].abs() + 1)
+    ml, my2, _ = reference(dict(m, z=f["z"]), sp, set(drop) | {"z"})
+    (my2 * (f["dy"].abs() * k)).sum().backward()
+    x = dict(zip(N.ScanGrads._fields, g))
+    pairs = (("du", "u"), ("ddelta", "delta"), ("dA", "A"), ("dB", "B"), ("dC", "C"), ("dD", "D"), ("dz", "z"),
+             ("ddelta_bias", "bias"))
+    for gk, lk in pairs:
+        name = {"bias": "delta_bias"}.get(lk, lk)
+        if name in drop:
+            assert x[gk] is None, gk
+            continue
+        ref = leaf[lk].grad
+        if lk == "z":
+            mag = my * f["dy"].abs() * 1.1 * k
+        elif lk in ("delta", "bias", "A"):
+            # d(decay) has A's sign and d(input) the other: the terms' sizes add
+            mag = _decay_mag(m, f, sp, drop, k, lk)
+        else:
+            mag = ml[lk].grad.abs()
+        R.close(f"{what} {gk}", x[gk], ref, 2 * CHAIN, mag)
+    return y, last, g
+
+
+def _decay_mag(m, f, sp, drop, k, which):
+    """Sizes of the terms of ddelta, its bias and dA: the adjoint with magnitudes times both parts."""
+    u, A, B, C = m["u"], f["A"], m["B"], m["C"]
+    Bn, L, Dn = u.shape
+    group = torch.arange(Dn) // (Dn // B.shape[2])
+    raw = f["delta"] if "delta_bias" in drop else f["delta"] + f["bias"]
+    dt = R.softplus(raw) if sp else raw
+    slope = torch.sigmoid(raw) if sp else torch.ones_like(raw)
+    a = torch.exp(dt[..., None] * A)
+    h = torch.zeros(Bn, *A.shape, dtype=u.dtype) if "state" in drop else m["state"]
+    hs = []
+    for t in range(L):
+        hs.append(h)
+        h = a[:, t] * h + (dt[:, t].abs() * u[:, t])[..., None] * B[:, t, group]
+    lam = torch.zeros_like(h)
+    out, dA = torch.zeros_like(u), torch.zeros_like(A)
+    dyk = f["dy"].abs() * k
+    for t in reversed(range(L)):
+        lam = lam + C[:, t, group] * dyk[:, t, :, None]
+        moved = lam * a[:, t] * hs[t]
+        out[:, t] = ((moved * A.abs()).sum(-1) + (lam * B[:, t, group]).sum(-1) * u[:, t]) * slope[:, t]
+        dA += (moved * dt[:, t, :, None].abs()).sum(0)
+        lam = lam * a[:, t]
+    return {"delta": out, "bias": out.sum((0, 1)), "A": dA}[which]
+
+
+CASES = [(1, 1, 1, 1, 1), (2, 2, 3, 4, 1), (3, 5, 8, 8, 2), (2, 9, 64, 16, 1), (1, 17, 70, 16, 1), (2, 40, 130, 5, 1),
+         (2, 33, 260, 16, 2), (1, 24, 300, 3, 3), (2, 37, 48, 32, 1), (1, 50, 600, 32, 2), (3, 70, 100, 24, 1)]
+
+
+@pytest.mark.parametrize("dt", R.DTYPES, ids=str)
+@pytest.mark.parametrize("case", CASES, ids=str)
+def test_forward_and_backward(N, case, dt):
+    t = inputs(*case, dt)
+    for sp, drop in ((True, ()), (True, ("z", "lengths")), (True, ("D", "state", "delta_bias"))):
+        print(f"case scan {case} {dt} {drop}", flush=True)
+        check(N, t, sp, drop, f"{case}")
+    t["delta"] = (0.05 + 0.1 * t["delta"].abs()).to(dt)  # step sizes as they are
+    check(N, t, False, ("delta_bias",), f"{case} no softplus")
+
+
+@pytest.mark.parametrize("case,dt", [((1, 400, 64, 16, 1), torch.float32), ((2, 517, 96, 8, 1), torch.bfloat16),
+                                     ((2, 1030, 20, 4, 2), torch.float16), ((1, 300, 40, 32, 1), torch.float32)],
+                         ids=str)
+def test_windows_in_chunks(N, case, dt):
+    print(f"case scan chunks {case} {dt}", flush=True)
+    a = N.ScanArgs(N._CODES[dt], case[3], case[4], 1, *case[:3])
+    assert N.lib().fpde_selective_scan_workspace(a) > 0  # (it is split)
+    t = inputs(*case, dt)
+    t["lengths"][-1] = case[1] // 3
+    y, last, g = check(N, t, True, (), "chunks")
+    c = cuda(t)
+    args, opts = call(N, c)
+    g2 = N.fpde_selective_scan_bwd(c["dy"], *args, **opts)
+    for p, q in zip(g, g2):
+        assert torch.equal(p, q)
+    # in place
+    st = c["state"].clone()
+    y2 = N.fpde_selective_scan(*args, state_out=st, **dict(opts, state=st))
+    assert torch.equal(y2, y) and torch.equal(st, last)
+
+
+def test_many_sequences(N):
+    """More sequences than workgroup rows of partial sums."""
+    t = inputs(150, 6, 12, 4, 1, torch.float32)
+    check(N, t, True, (), "many")
+
+
+def test_steps_continue_a_window(N):
+    for dt in R.DTYPES:
+        for n, G in ((16, 1), (3, 2), (32, 1), (5, 1)):
+            print(f"case scan step {dt} {n} {G}", flush=True)
+            t = inputs(3, 12, 70, n, G, dt)
+            c, f = cuda(t), f64(t)
+            state = c["state"].clone()
+            _, ry, rh = reference(f, True, ("lengths",), grad=False)
+            m = mag_inputs(f)
+            _, my, mh = reference(m, True, ("lengths", "z"), grad=False)
+            for i in range(12):
+                y = N.fpde_selective_step(state, c["u"][:, i], c["delta"][:, i], c["A"], c["B"][:, i], c["C"][:, i],
+                                          D=c["D"], z=c["z"][:, i], delta_bias=c["bias"])
+                R.close("step", y, ry[:, i], CHAIN, (my * f["z"].abs())[:, i])
+            R.close("state", state, rh, CHAIN, mh)
+
+
+def test_levels_past_a_length_are_not_read(N):
+    t = inputs(5, 60, 40, 16, 1, torch.float32)
+    t["lengths"] = torch.tensor([0, 1, 8, 17, 60], dtype=torch.int32)
+    c = cuda(t)
+    past = (torch.arange(60, device="cuda")[None] >= c["lengths"][:, None])[..., None]
+    args, opts = call(N, c)
+    last = torch.empty_like(c["state"])
+    y = N.fpde_selective_scan(*args, state_out=last, **opts)
+    assert not y.masked_select(past).any() and torch.equal(last[0], c["state"][0])
+    g = N.fpde_selective_scan_bwd(c["dy"], *args, **opts)
+    bad = dict(c)
+    for k in ("u", "delta", "z", "dy"):
+        bad[k] = c[k].masked_fill(past, float("nan"))
+    for k in ("B", "C"):
+        bad[k] = c[k].masked_fill(past[..., None], float("nan"))
+    args, opts = call(N, bad, lengths=torch.tensor([-5, 1, 8, 17, 99], dtype=torch.int32, device="cuda"))
+    assert torch.equal(N.fpde_selective_scan(*args, **opts), y)
+    for a, b in zip(N.fpde_selective_scan_bwd(bad["dy"], *args, **opts), g):
+        assert torch.equal(a, b)
+    for k in (g.du, g.ddelta, g.dz):
+        assert not k.masked_select(past).any()
+    assert not g.dB.masked_select(past[..., None]).any() and not g.dC.masked_select(past[..., None]).any()
+
+
+def test_extreme_steps(N):
+    """delta far out: no step (softplus underflows), a step that forgets everything; NaN stays in its channel."""
+    t = inputs(2, 20, 24, 4, 1, torch.float32)
+    t["delta"][0, 3, :8] = -200.0
+    t["delta"][0, 4, 8:16] = 300.0
+    t["delta"][1, 5, 0], t["delta"][1, 6, 1] = float("-inf"), -87.0
+    check(N, t, True, ("lengths",), "extreme")
+    t["u"][0, 2, 20] = float("nan")
+    c = cuda(t)
+    args, opts = call(N, c)
+    y = N.fpde_selective_scan(*args, **dict(opts, lengths=None)).cpu()
+    assert torch.isnan(y[0, 2:, 20]).all() and int(torch.isnan(y).sum()) == 18
+
+
+def test_strides_streams_and_graph(N):
+    t = cuda(inputs(2, 40, 72, 16, 2, torch.bfloat16))
+    args, opts = call(N, t)
+    y = N.fpde_selective_scan(*args, **opts)
+    g = N.fpde_selective_scan_bwd(t["dy"], *args, **opts)
+    both = torch.empty(2, 40, 2 * 72 + 1, device="cuda", dtype=torch.bfloat16)  # one projection's output
+    both[..., 1:73], both[..., 73:] = t["u"], t["z"]
+    bc = torch.empty(40, 2, 70, device="cuda", dtype=torch.bfloat16).transpose(0, 1)
+    bc[..., 3:35], bc[..., 35:67] = t["B"].flatten(2), t["C"].flatten(2)
+    s = dict(t, u=both[..., 1:73], z=both[..., 73:], B=bc[..., 3:35].unflatten(-1, (2, 16)),
+             C=bc[..., 35:67].unflatten(-1, (2, 16)))
+    args, opts = call(N, s)
+    assert torch.equal(N.fpde_selective_scan(*args, **opts), y)
+    for a, b in zip(N.fpde_selective_scan_bwd(s["dy"], *args, **opts), g):
+        assert torch.equal(a, b)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    g2 = N.fpde_selective_scan_bwd(s["dy"], *args, stream=side, **opts)
+    torch.cuda.current_stream().wait_stream(side)
+    for a, b in zip(g2, g):
+        assert torch.equal(a, b)
+    t = cuda(inputs(1, 300, 64, 16, 1, torch.float32))  # split in chunks
+    args, opts = call(N, t)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        gy = N.fpde_selective_scan(*args, **opts)
+        gg = N.fpde_selective_scan_bwd(t["dy"], *args, **opts)
+    for _ in range(3):
+        t["u"].mul_(0.5)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(gy, N.fpde_selective_scan(*args, **opts))
+        for a, b in zip(gg, N.fpde_selective_scan_bwd(t["dy"], *args, **opts)):
+            assert torch.equal(a, b)
+
+
+def test_no_sequences_and_no_levels(N):
+    A, D = -torch.ones(6, 4, device="cuda"), torch.ones(6, device="cuda")
+    for b, L in ((0, 5), (3, 0)):
+        u, bc = torch.empty(b, L, 6, device="cuda"), torch.empty(b, L, 4, device="cuda")
+        st = torch.randn(b, 6, 4, device="cuda")
+        out = torch.empty_like(st)
+        assert N.fpde_selective_scan(u, u, A, bc, bc, D=D, z=u, state=st, state_out=out).shape == (b, L, 6)
+        assert torch.equal(out, st)
+        g = N.fpde_selective_scan_bwd(u, u, u, A, bc, bc, D=D, z=u, state=st)
+        assert g.du.shape == (b, L, 6) and not g.dA.any() and not g.dD.any() and g.dB.shape == (b, L, 4)
+
+
+def test_autograd_and_differences(N):
+    t = inputs(2, 25, 12, 4, 1, torch.float32)
+    c = cuda(t)
+    leaf = {k: c[k].clone().requires_grad_() for k in NAMES}
+    rest = (True, c["state"], c["lengths"])
+    N.SelectiveScan.apply(*[leaf[k] for k in NAMES], *rest).backward(c["dy"])
+    g = torch.Generator().manual_seed(1)
+    h = 2.0 ** -9
+    for k in NAMES:
+        v = R.randn(g, *leaf[k].shape).cuda()
+        f = []
+        for sgn in (1, -1):
+            a = {q: leaf[q].detach() for q in NAMES}
+            a[k] = a[k] + sgn * h * v
+            with torch.no_grad():
+                y = N.SelectiveScan.apply(*[a[q] for q in NAMES], *rest)
+            f.append(float((y.double() * c["dy"]).sum()))
+        want = float((leaf[k].grad.double() * v).sum())
+        # 600 terms: truncation h^2 / 6 times third derivatives of up to about 100 (the decays' in A and
+        # delta), rounding 2^-24 times terms of up to about 16
+        assert abs((f[0] - f[1]) / (2 * h) - want) <= 600 * h * h * 100 / 6 + 600 * 16 * 2.0 ** -24 / h, k
+    with pytest.raises(ValueError):
+        N.SelectiveScan.apply(*[leaf[k] for k in NAMES], True, c["state"].clone().requires_grad_(), None)
