@@ -254,6 +254,57 @@ typedef struct fpde_scan_bwd_args {
 int64_t fpde_selective_scan_bwd_workspace(const fpde_scan_bwd_args* a); /* (reads sizes and types) */
 int fpde_selective_scan_bwd(const fpde_scan_bwd_args* a, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Newton-Schulz orthogonalisation: out = X after `steps` times
+ *     X0 = g / (|g|_F + eps);   A = X X^T,   X <- a X + (b A + c A^2) X
+ * (from the right, X^T X, where that is smaller), which drives every singular value
+ * of g towards 1.  `count` matrices of one shape [m][n], each dense, given by HOST
+ * arrays of device pointers.  float32 accuracy throughout: the products run on the
+ * matrix cores in pairs of float16 that hold 22 bits of each operand.  The iterates
+ * have to stay below 15 in magnitude (with the customary coefficients they stay below
+ * 1.3); past that they overflow to Inf or NaN.  A zero matrix gives zeros.
+ *
+ * Limits: 0 <= count <= 65536, 1 <= m, n <= 32768 (FPDE_ERR_SHAPE), 1 <= steps <= 100,
+ * coefficients and eps finite, eps >= 0 (FPDE_ERR_COEFF). */
+typedef struct fpde_ortho_args {
+    int32_t dtype;            /* g and out */
+    int32_t steps;
+    int64_t count, m, n;
+    double a, b, c;
+    double eps;
+    const void* const* g;
+    void* const* out;         /* out[i] may be g[i] */
+    void* workspace;
+    int64_t workspace_bytes;
+} fpde_ortho_args;
+
+int64_t fpde_orthogonalize_workspace(const fpde_ortho_args* a); /* (reads sizes, steps and types) */
+int fpde_orthogonalize(const fpde_ortho_args* a, void* stream);
+
+/* One step of the Muon optimiser for `count` weight matrices of one shape:
+ *     momentum <- mu * momentum + grad
+ *     u = grad + mu * momentum (nesterov) or momentum
+ *     weight <- (1 - lr * weight_decay) * weight - lr * scale * orthogonalize(u)
+ * momentum and weight are updated in place; sums in float32, weight rounded once. */
+typedef struct fpde_muon_args {
+    int32_t dtype;            /* grads and weights; momenta are float32 */
+    int32_t steps;
+    int32_t nesterov;         /* 0 or 1 */
+    int32_t reserved;         /* 0 */
+    int64_t count, m, n;
+    double a, b, c;
+    double eps;
+    double lr, mu, weight_decay, scale; /* finite (FPDE_ERR_COEFF) */
+    const void* const* grads;
+    float* const* momenta;
+    void* const* weights;
+    void* workspace;
+    int64_t workspace_bytes;
+} fpde_muon_args;
+
+int64_t fpde_muon_step_workspace(const fpde_muon_args* a); /* (reads sizes, steps and types) */
+int fpde_muon_step(const fpde_muon_args* a, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -57,7 +57,7 @@ CHECK_FLAGS = [
 # parallel, in a library of its own.
 NET_LIB = os.path.join(PKG, "libfpde_net.so")
 NET_DIR = os.path.join(HERE, "net")
-NET_SOURCES = [os.path.join(NET_DIR, f) for f in ("norm.hip", "conv.hip", "scan.hip")]
+NET_SOURCES = [os.path.join(NET_DIR, f) for f in ("norm.hip", "conv.hip", "scan.hip", "ortho.hip")]
 
 _NOISE = "is not a recognized feature for this target"
 

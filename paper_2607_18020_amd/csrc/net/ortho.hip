@@ -1,0 +1,654 @@
+// ortho.hip -- Newton-Schulz orthogonalisation of matrices, and the Muon step.
+//
+//   X0 = u / (|u|_F + eps);  k times: A = X X^T, B = b A + c A^2, X <- a X + B X
+//
+// with X held such that its rows are the shorter side: s rows, l columns.  A and A^2
+// are symmetric, so one triangle of their tiles is computed and written twice:
+// s^2 l + s^3 + 2 s^2 l flops a step.
+//
+// Precision.  The iteration multiplies what the smallest singular directions hold by a^k
+// (about 500 for five customary steps), rounding errors included, so products of
+// plain 16-bit operands would lose those directions.  Every operand v is kept as two
+// float16, hi = f16(S v) and lo = f16(S v - hi), S = 2^12: 22 bits together, and
+// their product as hi hi + hi lo + lo hi in the matrix cores' float32 sums; lo lo
+// is below float32's own rounding.  Three f16 products cost 3/16 of the f32 matrix
+// instructions' time.  The term a X stays outside the product (a + B in one matrix
+// would round B against a).  S leaves entries up to 15 representable, and keeps the
+// low halves of entries down to 2^-13 out of the subnormals.
+//
+// Small matrices (s <= 128 and l <= 128, or s <= 64 and l <= 256): one workgroup and one
+// launch for a whole matrix, momentum and weight update included.  X stays in
+// registers; X, A, B take turns in two LDS regions.  What bounds it is the LDS reads
+// of the operands.
+//
+// Others: each product is a launch of a tiled kernel over all matrices.  Both operands
+// of every product are rows that are contiguous along the sum (A and A^2 are
+// symmetric, and X is kept in both orders), so tiles go from memory to LDS by
+// direct loads, 16 bytes a lane, and from there to the matrix cores by 16-byte reads;
+// the chunks of a row are permuted such that those reads meet no bank twice.
+#include <stdlib.h>
+
+#include "net_common.hpp"
+
+using namespace fpde_net;
+
+namespace {
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr float kS = 4096.f, kInvS = 1.f / 4096.f, kInvSS = kInvS * kInvS;
+
+__device__ __forceinline__ void split(float v, f16& hi, f16& lo) {
+    const float t = v * kS;
+    hi = (f16)t;
+    lo = (f16)(t - (float)hi);
+}
+
+constexpr int kMaxCount = 32;  // matrices of one launch
+
+// The matrices of one launch and what becomes of them.
+struct Mats {
+    const void* g[kMaxCount];
+    float* mom[kMaxCount];     // Muon: the momenta; else unused
+    void* out[kMaxCount];      // the result, or the weights
+    int m, n;                  // stored shape
+    int tall;                  // X = u^T
+    int muon, nesterov;
+    float mu, keep, rate;      // weight <- keep * weight - rate * X
+    float eps;
+};
+
+// u of element i, the momentum brought up to date (update) or read as it is now
+template <class T>
+__device__ __forceinline__ float update_of(const Mats& M, int mat, int64_t i, bool update) {
+    const float g = to_f32<T>(((const T*)M.g[mat])[i]);
+    if (!M.muon) return g;
+    float m = M.mom[mat][i];
+    if (update) {
+        m = fmaf(M.mu, m, g);
+        M.mom[mat][i] = m;
+    }
+    return M.nesterov ? fmaf(M.mu, m, g) : m;
+}
+
+template <class T>
+__device__ __forceinline__ void finish(const Mats& M, int mat, int64_t i, float x) {
+    T* o = (T*)M.out[mat] + i;
+    *o = from_f32<T>(M.muon ? fmaf(M.keep, to_f32<T>(*o), -M.rate * x) : x);
+}
+
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o, 64);
+    return v;
+}
+
+// 1 / (|u|_F + eps) from the sum of squares (double: no overflow, no underflow of squares)
+__device__ __forceinline__ float inv_norm(double sumsq, float eps) {
+    const double d = sqrt(sumsq) + (double)eps, r = 1.0 / d;
+    return d == 0.0 ? 0.f : (r > 3.4e38 ? 3.4e38f : (float)r);
+}
+
+// ---------------------------------------------------------------------------
+// Small matrices.
+
+// Products of rows of U and rows of V, both [rows][pitch] in LDS, hi then lo `half`
+// elements later: MT x NT tiles of 16 x 16.  A lane reads 8 neighbouring k of row l % 16.
+template <int MT, int NT>
+__device__ __forceinline__ void lds_product(f32x4 (&acc)[MT][NT], const f16* U, int pu, int hu, const f16* V,
+                                            int pv, int hv, int K) {
+    const int lane = (int)(threadIdx.x & 63), r = lane & 15, k0 = (lane >> 4) * 8;
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int k = k0; k < K; k += 32) {
+        f16x8 uh[MT], ul[MT], vh[NT], vl[NT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            uh[i] = *(const f16x8*)(U + (i * 16 + r) * pu + k);
+            ul[i] = *(const f16x8*)(U + hu + (i * 16 + r) * pu + k);
+        }
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            vh[j] = *(const f16x8*)(V + (j * 16 + r) * pv + k);
+            vl[j] = *(const f16x8*)(V + hv + (j * 16 + r) * pv + k);
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(uh[i], vl[j], acc[i][j], 0, 0, 0);
+                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ul[i], vh[j], acc[i][j], 0, 0, 0);
+                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(uh[i], vh[j], acc[i][j], 0, 0, 0);
+            }
+    }
+}
+
+// Four neighbouring k of row `row` (the four rows of one column of a result tile)
+__device__ __forceinline__ void put4(f16* p, int half, const float (&v)[4]) {
+    f16x4 h, l;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        f16 a, b;
+        split(v[e], a, b);
+        h[e] = a, l[e] = b;
+    }
+    *(f16x4*)p = h;
+    *(f16x4*)(p + half) = l;
+}
+
+// One workgroup of 8 wavefronts, 2 x 4 of them over the rows and columns of X, a matrix.
+template <class T, int SP, int LP>
+__global__ __launch_bounds__(512) void ortho_small_kernel(Mats M, int steps, float ca, float cb, float cc) {
+    constexpr int PS = SP + 8, PL = LP + 8;                // pitches: rows 16 bytes apart in the banks
+    constexpr int HR = SP * PL, HT = LP * PS, HA = SP * PS;  // elements of X, X^T, A or B
+    constexpr int R1 = HR > HA ? HR : HA, R2 = HT > HA ? HT : HA;
+    static_assert((R1 + R2) * 4 + 64 <= 160 * 1024, "LDS");
+    __shared__ __attribute__((aligned(16))) f16 lds1[2 * R1];
+    __shared__ __attribute__((aligned(16))) f16 lds2[2 * R2];
+    __shared__ double sums[8];
+    constexpr int MT = SP / 32, NT = LP / 64, AT = SP / 64;
+    const int mat = (int)blockIdx.x, lane = (int)(threadIdx.x & 63), wave = (int)(threadIdx.x >> 6);
+    const int row0 = (wave >> 2) * (SP / 2), col0 = (wave & 3) * (LP / 4), acol0 = (wave & 3) * (SP / 4);
+    const int r4 = (lane >> 4) * 4, cl = lane & 15;
+    const int s = M.tall ? M.n : M.m, l = M.tall ? M.m : M.n;
+    // element (row, col) of X in the stored matrix
+    auto index = [&](int row, int col) {
+        return M.tall ? (int64_t)col * M.n + row : (int64_t)row * M.n + col;
+    };
+    float x[MT][NT][4];
+    double ss = 0.0;
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int row = row0 + i * 16 + r4 + e, col = col0 + j * 16 + cl;
+                x[i][j][e] = row < s && col < l ? update_of<T>(M, mat, index(row, col), true) : 0.f;
+                ss += (double)x[i][j][e] * (double)x[i][j][e];
+            }
+    ss = wave_sum(ss);
+    if (lane == 0) sums[wave] = ss;
+    __syncthreads();
+    ss = sums[0];
+#pragma unroll
+    for (int w = 1; w < 8; ++w) ss += sums[w];
+    const float inv = inv_norm(ss, M.eps);
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[i][j][e] *= inv;
+    for (int it = 0; it < steps; ++it) {
+        // X by rows
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    f16* p = lds1 + (row0 + i * 16 + r4 + e) * PL + col0 + j * 16 + cl;
+                    split(x[i][j][e], p[0], p[R1]);
+                }
+        __syncthreads();
+        f32x4 acc[MT][AT];
+        lds_product<MT, AT>(acc, lds1 + row0 * PL, PL, R1, lds1 + acol0 * PL, PL, R1, LP);
+        float A[MT][AT][4];
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < AT; ++j) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) A[i][j][e] = acc[i][j][e] * kInvSS;
+                put4(lds2 + (acol0 + j * 16 + cl) * PS + row0 + i * 16 + r4, R2, A[i][j]);  // (symmetric)
+            }
+        __syncthreads();
+        lds_product<MT, AT>(acc, lds2 + row0 * PS, PS, R2, lds2 + acol0 * PS, PS, R2, SP);
+        // (every wavefront is past its reads of X by rows: B takes its place)
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < AT; ++j) {
+                float b[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) b[e] = fmaf(cb, A[i][j][e], cc * kInvSS * acc[i][j][e]);
+                put4(lds1 + (acol0 + j * 16 + cl) * PS + row0 + i * 16 + r4, R1, b);
+            }
+        __syncthreads();  // (and past those of A: X by columns takes its place)
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+                put4(lds2 + (col0 + j * 16 + cl) * PS + row0 + i * 16 + r4, R2, x[i][j]);
+        __syncthreads();
+        f32x4 y[MT][NT];
+        lds_product<MT, NT>(y, lds1 + row0 * PS, PS, R1, lds2 + col0 * PS, PS, R2, SP);
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[i][j][e] = fmaf(ca, x[i][j][e], y[i][j][e] * kInvSS);
+        __syncthreads();
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int row = row0 + i * 16 + r4 + e, col = col0 + j * 16 + cl;
+                if (row < s && col < l) finish<T>(M, mat, index(row, col), x[i][j][e]);
+            }
+}
+
+// ---------------------------------------------------------------------------
+// Large matrices.
+
+constexpr int kNormBlocks = 256;  // partial sums of squares a matrix
+
+template <class T>
+__global__ __launch_bounds__(256) void ortho_norm_kernel(Mats M, double* part) {
+    __shared__ double red[4];
+    const int mat = (int)blockIdx.y;
+    const int64_t n = (int64_t)M.m * M.n;
+    double ss = 0.0;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)kNormBlocks * 256) {
+        const float v = update_of<T>(M, mat, i, true);
+        ss += (double)v * (double)v;
+    }
+    ss = wave_sum(ss);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = ss;
+    __syncthreads();
+    if (threadIdx.x == 0) part[mat * kNormBlocks + blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+// Halves of one [rows][cols] matrix of all matrices of a launch, `step` elements apart.
+struct Half {
+    f16 *hi, *lo;
+    int64_t step;
+    int ld;
+};
+
+// X0 in both orders, zeros in the padding.  64 x 64 tiles of X; 256 threads.
+template <class T>
+__global__ __launch_bounds__(256) void ortho_split_kernel(Mats M, const double* part, Half X, Half Xt) {
+    __shared__ float tile[64][65];
+    __shared__ double red[4];
+    const int mat = (int)blockIdx.z, lane = (int)(threadIdx.x & 63), wave = (int)(threadIdx.x >> 6);
+    double ss = wave_sum(part[mat * kNormBlocks + threadIdx.x]);
+    if (lane == 0) red[wave] = ss;
+    __syncthreads();
+    ss = (red[0] + red[1]) + (red[2] + red[3]);
+    const float inv = inv_norm(ss, M.eps);
+    const int r0 = (int)blockIdx.y * 64, c0 = (int)blockIdx.x * 64;
+    const int s = M.tall ? M.n : M.m, l = M.tall ? M.m : M.n;
+    for (int i = wave; i < 64; i += 4) {
+        // neighbouring lanes read neighbouring elements of the stored matrix
+        const int row = M.tall ? r0 + lane : r0 + i, col = M.tall ? c0 + i : c0 + lane;
+        float v = 0.f;
+        if (row < s && col < l)
+            v = inv * update_of<T>(M, mat, M.tall ? (int64_t)col * M.n + row : (int64_t)row * M.n + col, false);
+        if (M.tall)
+            tile[lane][i] = v;
+        else
+            tile[i][lane] = v;
+    }
+    __syncthreads();
+    for (int i = wave; i < 64; i += 4) {
+        const int64_t a = mat * X.step + (int64_t)(r0 + i) * X.ld + c0 + lane;
+        split(tile[i][lane], X.hi[a], X.lo[a]);
+        const int64_t b = mat * Xt.step + (int64_t)(c0 + i) * Xt.ld + r0 + lane;
+        split(tile[lane][i], Xt.hi[b], Xt.lo[b]);
+    }
+}
+
+// C = ca Z + cp U V^T for [M][K] U and [N][K] V; C in both orders, or into the results.
+struct Prod {
+    Half U, V, Z, C, Ct;
+    int tm, tn, K;       // tiles over the rows and columns of C; the sum's length, a multiple of 32
+    int sym;             // C is square and symmetric: tiles on and above the diagonal, Ct = C
+    float ca, cp;
+};
+
+// tile i of the upper triangle of t x t tiles, by rows
+__device__ __forceinline__ void triangle(int i, int t, int* r, int* c) {
+    int row = 0;
+    while (i >= t - row) i -= t - row, ++row;
+    *r = row, *c = row + i;
+}
+
+typedef const __attribute__((address_space(1))) void* gptr_t;
+typedef __attribute__((address_space(3))) void* lptr_t;
+
+template <int TILE, bool LAST, class T>
+__global__ __launch_bounds__(256) void ortho_product_kernel(Prod P, Mats M) {
+    constexpr int CH = TILE * 4;                       // 16-byte chunks of a TILE x 32 operand tile
+    constexpr int W = TILE / 2, F = W / 32;            // a wavefront's share, in 32 x 32 tiles
+    constexpr int STAGE = 4 * CH;                      // chunks: U hi, U lo, V hi, V lo
+    constexpr int OUT = TILE * (TILE + 1) * 4;         // the result tile in float32
+    constexpr int BYTES = 2 * STAGE * 16 > OUT ? 2 * STAGE * 16 : OUT;
+    __shared__ __attribute__((aligned(16))) char lds[BYTES];
+    const int mat = (int)blockIdx.y, lane = (int)(threadIdx.x & 63);
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    int tr, tc;
+    if (P.sym)
+        triangle((int)blockIdx.x, P.tm, &tr, &tc);
+    else
+        tr = (int)blockIdx.x % P.tm, tc = (int)blockIdx.x / P.tm;
+    const f16* src[4] = {P.U.hi + mat * P.U.step + (int64_t)tr * TILE * P.U.ld,
+                         P.U.lo + mat * P.U.step + (int64_t)tr * TILE * P.U.ld,
+                         P.V.hi + mat * P.V.step + (int64_t)tc * TILE * P.V.ld,
+                         P.V.lo + mat * P.V.step + (int64_t)tc * TILE * P.V.ld};
+    // Chunk q of a tile holds row q / 4; of the row's four chunks of 8 k it is number (q % 4) ^ (row / 4 % 4),
+    // so that 16 rows' chunks of one k lie in different banks.
+    auto fetch = [&](int k, int buf) {
+#pragma unroll
+        for (int o = 0; o < 4; ++o)
+#pragma unroll
+            for (int i = 0; i < CH / 256; ++i) {
+                const int q0 = i * 256 + wave * 64, q = q0 + lane, row = q >> 2, ch = (q & 3) ^ ((row >> 2) & 3);
+                const f16* g = src[o] + (int64_t)row * (o < 2 ? P.U.ld : P.V.ld) + k + ch * 8;
+                __builtin_amdgcn_global_load_lds((gptr_t)g, (lptr_t)(lds + ((buf * 4 + o) * CH + q0) * 16), 16, 0,
+                                                 0);
+            }
+    };
+    const int wr = (wave >> 1) * W, wc = (wave & 1) * W, r = lane & 31, kh = lane >> 5;
+    auto operand = [&](int o, int buf, int row, int ch) {
+        return *(const f16x8*)(lds + ((buf * 4 + o) * CH + row * 4 + (ch ^ ((row >> 2) & 3))) * 16);
+    };
+    f32x16 acc[F][F];
+#pragma unroll
+    for (int i = 0; i < F; ++i)
+#pragma unroll
+        for (int j = 0; j < F; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+    fetch(0, 0);
+    int buf = 0;
+    for (int k = 0; k < P.K; k += 32, buf ^= 1) {
+        __builtin_amdgcn_s_waitcnt(0);  // this wavefront's part of the tile is in LDS
+        __syncthreads();                // everyone's is, and nobody reads the other buffer any more
+        if (k + 32 < P.K) fetch(k + 32, buf ^ 1);
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            f16x8 uh[F], ul[F], vh[F], vl[F];
+#pragma unroll
+            for (int i = 0; i < F; ++i) {
+                uh[i] = operand(0, buf, wr + i * 32 + r, kk * 2 + kh);
+                ul[i] = operand(1, buf, wr + i * 32 + r, kk * 2 + kh);
+                vh[i] = operand(2, buf, wc + i * 32 + r, kk * 2 + kh);
+                vl[i] = operand(3, buf, wc + i * 32 + r, kk * 2 + kh);
+            }
+#pragma unroll
+            for (int i = 0; i < F; ++i)
+#pragma unroll
+                for (int j = 0; j < F; ++j) {
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(uh[i], vl[j], acc[i][j], 0, 0, 0);
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ul[i], vh[j], acc[i][j], 0, 0, 0);
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(uh[i], vh[j], acc[i][j], 0, 0, 0);
+                }
+        }
+    }
+    // The tile by way of LDS, so that both orders are written along their rows.
+    __syncthreads();
+    float* t = (float*)lds;
+    constexpr int PT = TILE + 1;
+#pragma unroll
+    for (int i = 0; i < F; ++i)
+#pragma unroll
+        for (int j = 0; j < F; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                t[(wr + i * 32 + (e & 3) + 8 * (e >> 2) + 4 * kh) * PT + wc + j * 32 + r] = acc[i][j][e] * P.cp;
+    __syncthreads();
+    for (int q = (int)threadIdx.x; q < TILE * TILE; q += 256) {
+        const int row = q / TILE, col = q % TILE;
+        float v = t[row * PT + col];
+        if (P.Z.hi) {
+            const int64_t z = mat * P.Z.step + (int64_t)(tr * TILE + row) * P.Z.ld + tc * TILE + col;
+            v = fmaf(P.ca * kInvS, (float)P.Z.hi[z] + (float)P.Z.lo[z], v);
+        }
+        if constexpr (LAST) {
+            if (M.tall) {
+                t[row * PT + col] = v;
+            } else if (tr * TILE + row < M.m && tc * TILE + col < M.n) {
+                finish<T>(M, mat, (int64_t)(tr * TILE + row) * M.n + tc * TILE + col, v);
+            }
+        } else {
+            const int64_t c = mat * P.C.step + (int64_t)(tr * TILE + row) * P.C.ld + tc * TILE + col;
+            split(v, P.C.hi[c], P.C.lo[c]);
+            t[row * PT + col] = v;
+        }
+    }
+    if (LAST ? !M.tall : (P.sym && tr == tc)) return;
+    __syncthreads();
+    for (int q = (int)threadIdx.x; q < TILE * TILE; q += 256) {
+        const int col = q / TILE, row = q % TILE;
+        const float v = t[row * PT + col];
+        if constexpr (LAST) {
+            if (tc * TILE + col < M.m && tr * TILE + row < M.n)
+                finish<T>(M, mat, (int64_t)(tc * TILE + col) * M.n + tr * TILE + row, v);
+        } else {
+            const int64_t c = mat * P.Ct.step + (int64_t)(tc * TILE + col) * P.Ct.ld + tr * TILE + row;
+            split(v, P.Ct.hi[c], P.Ct.lo[c]);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Host side.
+
+// Bytes of workspace that a batch of large matrices may take together.
+constexpr int64_t kBatchBytes = (int64_t)1 << 30;
+
+struct OrthoPlan {
+    int s, l;              // rows and columns of X
+    int small;             // padded l of the one-workgroup kernel, or 0
+    int tile;
+    int64_t sp, lp;        // padded
+    int64_t batch;         // matrices of a launch
+    int64_t bytes;
+};
+
+OrthoPlan plan(int64_t count, int64_t m, int64_t n) {
+    OrthoPlan p;
+    p.s = (int)(m < n ? m : n), p.l = (int)(m < n ? n : m);
+    p.small = p.s <= 64 && p.l <= 64 ? 64 : p.s <= 64 && p.l <= 256 ? (p.l <= 128 ? 128 : 256)
+              : p.l <= 128         ? 128 : 0;
+    p.batch = kMaxCount, p.bytes = 0, p.tile = 0, p.sp = p.lp = 0;
+    if (p.small) return p;
+    // Tiles of 128 need half the reads of 64 a flop, but only where there are enough of them for
+    // every compute unit.
+    const int64_t t = cdiv(p.s, 128);
+    p.tile = t * (t + 1) / 2 * (count < 1 ? 1 : count) >= 256 ? 128 : 64;
+    p.sp = cdiv(p.s, p.tile) * p.tile, p.lp = cdiv(p.l, p.tile) * p.tile;
+    // X and X^T twice (a step reads one and writes the other), A, B: hi and lo of each
+    const int64_t each = (4 * p.sp * p.lp + 2 * p.sp * p.sp) * 4;
+    p.batch = kBatchBytes / each;
+    p.batch = p.batch < 1 ? 1 : (p.batch > kMaxCount ? kMaxCount : p.batch);
+    if (p.batch > count) p.batch = count < 1 ? 1 : count;
+    p.bytes = p.batch * (each + kNormBlocks * (int64_t)sizeof(double));
+    return p;
+}
+
+bool is_finite(double v) { return v - v == 0.0; }
+
+int check_ortho(int dtype, int steps, int64_t count, int64_t m, int64_t n, double a, double b, double c,
+                double eps) {
+    if (size_of(dtype) == 0) return FPDE_ERR_UNSUPPORTED;
+    if (count < 0 || count > 65536 || m < 1 || n < 1 || m > 32768 || n > 32768) return FPDE_ERR_SHAPE;
+    if (steps < 1 || steps > 100 || !is_finite(a) || !is_finite(b) || !is_finite(c) || !is_finite(eps) || eps < 0.0)
+        return FPDE_ERR_COEFF;
+    return FPDE_OK;
+}
+
+// In steps of one launch's matrices; M holds what is common to all.
+template <class T>
+int run_large(const Mats& M, const OrthoPlan& p, int count, int steps, float ca, float cb, float cc, void* ws,
+              hipStream_t s) {
+    char* at = (char*)ws;
+    double* part = (double*)at;
+    at += p.batch * kNormBlocks * (int64_t)sizeof(double);
+    auto half = [&](int64_t rows, int64_t cols) {
+        Half h;
+        h.hi = (f16*)at, h.step = rows * cols, h.ld = (int)cols;
+        h.lo = h.hi + p.batch * rows * cols;
+        at += p.batch * rows * cols * 4;
+        return h;
+    };
+    Half X[2], Xt[2];
+    for (int i = 0; i < 2; ++i) X[i] = half(p.sp, p.lp), Xt[i] = half(p.lp, p.sp);
+    const Half A = half(p.sp, p.sp), B = half(p.sp, p.sp);
+    int r = launch(ortho_norm_kernel<T>, dim3(kNormBlocks, count), dim3(256), s, M, part);
+    if (r == FPDE_OK)
+        r = launch(ortho_split_kernel<T>, dim3((unsigned)(p.lp / 64), (unsigned)(p.sp / 64), count), dim3(256), s,
+                   M, part, X[0], Xt[0]);
+    const int ts = (int)(p.sp / p.tile), tl = (int)(p.lp / p.tile);
+    auto product = [&](const Prod& P, bool last) {
+        const dim3 g((unsigned)(P.sym ? ts * (ts + 1) / 2 : P.tm * P.tn), count), b(256);
+        if (p.tile == 128)
+            return last ? launch(ortho_product_kernel<128, true, T>, g, b, s, P, M)
+                        : launch(ortho_product_kernel<128, false, float>, g, b, s, P, M);
+        return last ? launch(ortho_product_kernel<64, true, T>, g, b, s, P, M)
+                    : launch(ortho_product_kernel<64, false, float>, g, b, s, P, M);
+    };
+    const Half none{nullptr, nullptr, 0, 0};
+    for (int i = 0; i < steps && r == FPDE_OK; ++i) {
+        const int o = i & 1;
+        r = product(Prod{X[o], X[o], none, A, A, ts, ts, (int)p.lp, 1, 0.f, kInvSS}, false);
+        if (r == FPDE_OK) r = product(Prod{A, A, A, B, B, ts, ts, (int)p.sp, 1, cb, cc * kInvSS}, false);
+        if (r == FPDE_OK)
+            r = product(Prod{B, Xt[o], X[o], X[o ^ 1], Xt[o ^ 1], ts, tl, (int)p.sp, 0, ca, kInvSS},
+                        i + 1 == steps);
+    }
+    return r;
+}
+
+template <class A>
+int run_ortho(const A* a, Mats M, const OrthoPlan& p, const void* const* g, float* const* mom, void* const* out,
+              void* stream) {
+    M.m = (int)a->m, M.n = (int)a->n, M.tall = a->m > a->n, M.eps = (float)a->eps;
+    const float ca = (float)a->a, cb = (float)a->b, cc = (float)a->c;
+    hipStream_t s = (hipStream_t)stream;
+    for (int64_t first = 0; first < a->count; first += p.batch) {
+        const int n = (int)(a->count - first < p.batch ? a->count - first : p.batch);
+        for (int i = 0; i < n; ++i) {
+            M.g[i] = g[first + i], M.out[i] = out[first + i];
+            M.mom[i] = mom ? mom[first + i] : nullptr;
+        }
+        const int st = with_type(a->dtype, [&](auto t) {
+            using T = decltype(t);
+            const dim3 grid(n), block(512);
+            if (!p.small) return run_large<T>(M, p, n, a->steps, ca, cb, cc, a->workspace, s);
+            if (p.s > 64) return launch(ortho_small_kernel<T, 128, 128>, grid, block, s, M, a->steps, ca, cb, cc);
+            if (p.small == 64) return launch(ortho_small_kernel<T, 64, 64>, grid, block, s, M, a->steps, ca, cb, cc);
+            if (p.small == 128)
+                return launch(ortho_small_kernel<T, 64, 128>, grid, block, s, M, a->steps, ca, cb, cc);
+            return launch(ortho_small_kernel<T, 64, 256>, grid, block, s, M, a->steps, ca, cb, cc);
+        });
+        if (st != FPDE_OK) return st;
+    }
+    return FPDE_OK;
+}
+
+// Alignment and presence of every matrix, and that those written overlap no other: sorted by address,
+// each ends before the next begins (but for an in-place pair).
+struct Range {
+    uintptr_t p;
+    int64_t n;
+    int out, mat;
+};
+int by_address(const void* a, const void* b) {
+    const Range *x = (const Range*)a, *y = (const Range*)b;
+    return x->p != y->p ? (x->p < y->p ? -1 : 1) : y->out - x->out;  // (a written one first)
+}
+
+int check_ranges(Range* r, int64_t n, bool in_place) {
+    qsort(r, (size_t)n, sizeof(Range), by_address);
+    // end: of the furthest range so far, and of the furthest written one
+    uintptr_t end = 0, out_end = 0;
+    const Range* prev = nullptr;
+    for (int64_t i = 0; i < n; ++i) {
+        const bool pair = in_place && prev && prev->p == r[i].p && prev->n == r[i].n && prev->mat == r[i].mat;
+        if (!pair && (r[i].p < out_end || (r[i].out && r[i].p < end))) return FPDE_ERR_ARG;
+        const uintptr_t e = r[i].p + (uintptr_t)r[i].n;
+        if (e > end) end = e;
+        if (r[i].out && e > out_end) out_end = e;
+        prev = &r[i];
+    }
+    return FPDE_OK;
+}
+
+}  // namespace
+
+extern "C" int64_t fpde_orthogonalize_workspace(const fpde_ortho_args* a) {
+    if (!a) return FPDE_ERR_ARG;
+    const int st = check_ortho(a->dtype, a->steps, a->count, a->m, a->n, a->a, a->b, a->c, a->eps);
+    return st != FPDE_OK ? st : plan(a->count, a->m, a->n).bytes;
+}
+
+static int check_matrices(int dtype, int64_t count, int64_t m, int64_t n, const void* const* g, float* const* mom,
+                          void* const* out, const void* ws, int64_t ws_bytes, int64_t need, bool in_place) {
+    if (!g || !out) return FPDE_ERR_ARG;
+    if (need > 0 && (!ws || ws_bytes < need)) return FPDE_ERR_ARG;
+    if (need > 0 && (uintptr_t)ws % 16) return FPDE_ERR_ALIGN;
+    const int e = size_of(dtype);
+    for (int64_t i = 0; i < count; ++i) {
+        if (!g[i] || !out[i] || (mom && !mom[i])) return FPDE_ERR_ARG;
+        if ((uintptr_t)g[i] % e || (uintptr_t)out[i] % e || (mom && (uintptr_t)mom[i] % 4)) return FPDE_ERR_ALIGN;
+    }
+    Range* r = (Range*)malloc(sizeof(Range) * (size_t)(3 * count + 1));
+    if (!r) return FPDE_ERR_HIP;
+    int64_t k = 0;
+    for (int64_t i = 0; i < count; ++i) {
+        r[k++] = Range{(uintptr_t)g[i], m * n * e, 0, (int)i};
+        r[k++] = Range{(uintptr_t)out[i], m * n * e, 1, (int)i};
+        if (mom) r[k++] = Range{(uintptr_t)mom[i], m * n * 4, 1, (int)i};
+    }
+    if (need > 0) r[k++] = Range{(uintptr_t)ws, need, 1, -1};
+    const int st = check_ranges(r, k, in_place);
+    free(r);
+    return st;
+}
+
+extern "C" int fpde_orthogonalize(const fpde_ortho_args* a, void* stream) {
+    const int64_t need = fpde_orthogonalize_workspace(a);
+    if (need < 0) return (int)need;
+    if (a->count == 0) return FPDE_OK;
+    const int st = check_matrices(a->dtype, a->count, a->m, a->n, a->g, nullptr, a->out, a->workspace,
+                                  a->workspace_bytes, need, true);
+    if (st != FPDE_OK) return st;
+    Mats M{};
+    return run_ortho(a, M, plan(a->count, a->m, a->n), a->g, nullptr, a->out, stream);
+}
+
+extern "C" int64_t fpde_muon_step_workspace(const fpde_muon_args* a) {
+    if (!a) return FPDE_ERR_ARG;
+    const int st = check_ortho(a->dtype, a->steps, a->count, a->m, a->n, a->a, a->b, a->c, a->eps);
+    if (st != FPDE_OK) return st;
+    if (!is_finite(a->lr) || !is_finite(a->mu) || !is_finite(a->weight_decay) || !is_finite(a->scale)) return FPDE_ERR_COEFF;
+    if ((a->nesterov != 0 && a->nesterov != 1) || a->reserved != 0) return FPDE_ERR_ARG;
+    return plan(a->count, a->m, a->n).bytes;
+}
+
+extern "C" int fpde_muon_step(const fpde_muon_args* a, void* stream) {
+    const int64_t need = fpde_muon_step_workspace(a);
+    if (need < 0) return (int)need;
+    if (a->count == 0) return FPDE_OK;
+    if (!a->momenta) return FPDE_ERR_ARG;
+    const int st = check_matrices(a->dtype, a->count, a->m, a->n, a->grads, a->momenta, a->weights, a->workspace,
+                                  a->workspace_bytes, need, false);
+    if (st != FPDE_OK) return st;
+    Mats M{};
+    M.muon = 1, M.nesterov = a->nesterov;
+    M.mu = (float)a->mu;
+    M.keep = (float)(1.0 - a->lr * a->weight_decay), M.rate = (float)(a->lr * a->scale);
+    return run_ortho(a, M, plan(a->count, a->m, a->n), a->grads, a->momenta, a->weights, stream);
+}

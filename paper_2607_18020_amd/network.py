@@ -83,11 +83,21 @@ class ScanBwdArgs(ctypes.Structure):
                        "ddelta_bias workspace; i64 workspace_bytes")
 
 
+class OrthoArgs(ctypes.Structure):
+    _fields_ = _fields("i32 dtype steps; i64 count m n; f64 a b c eps; ptr g out workspace; i64 workspace_bytes")
+
+
+class MuonArgs(ctypes.Structure):
+    _fields_ = _fields("i32 dtype steps nesterov reserved; i64 count m n; f64 a b c eps lr mu weight_decay scale; "
+                       "ptr grads momenta weights workspace; i64 workspace_bytes")
+
+
 # entry points and their argument structs; those with a workspace also have a
 # function ending in _workspace
 CALLS = {"fpde_rms_norm": (NormArgs, False), "fpde_rms_norm_bwd": (NormBwdArgs, True),
          "fpde_causal_conv": (ConvArgs, False), "fpde_causal_conv_bwd": (ConvBwdArgs, True),
-         "fpde_selective_scan": (ScanArgs, True), "fpde_selective_scan_bwd": (ScanBwdArgs, True)}
+         "fpde_selective_scan": (ScanArgs, True), "fpde_selective_scan_bwd": (ScanBwdArgs, True),
+         "fpde_orthogonalize": (OrthoArgs, True), "fpde_muon_step": (MuonArgs, True)}
 EXPORTED = tuple(CALLS) + tuple(n + "_workspace" for n, (_, ws) in CALLS.items() if ws)
 
 _lib = None
@@ -515,3 +525,126 @@ class SelectiveScan(torch.autograd.Function):
         g = fpde_selective_scan_bwd(dy.contiguous(), u, delta, A, B, C, D=D, z=z, delta_bias=bias,
                                     softplus=ctx.softplus, state=state, lengths=lengths)
         return (*g, None, None, None)
+
+
+# ---------------------------------------------------------------------------
+# Orthogonalised updates.
+
+NS_COEFFS = (3.4445, -4.7750, 2.0315)
+
+
+def _matrices(what, ts, like=None, dtype=None):
+    """(tensors, host array of their pointers) of dense matrices of one shape, type and device."""
+    ts = list(ts)
+    t0 = ts[0] if like is None else like
+    shape, dt, dev = t0.shape, dtype or t0.dtype, t0.device
+    for t in ts:
+        _dense(what, t, shape, dt, dev)
+    return ts, (_vp * len(ts))(*[t.data_ptr() for t in ts])
+
+
+def fpde_orthogonalize(mats, *, steps: int = 5, coeffs=NS_COEFFS, eps: float = 1e-7, out=None, stream=None):
+    """Queue the Newton-Schulz orthogonalisation of matrices: X = g / (|g| + eps), then
+    ``steps`` times X <- a X + (b A + c A^2) X with A = X X^T.  ``mats``: a dense
+    [..., m, n] tensor, or a sequence of dense [m, n] tensors of one shape; returns the
+    same (``out``: where to, like ``mats``, or ``mats`` itself)."""
+    what = "fpde_orthogonalize"
+    one = isinstance(mats, torch.Tensor)
+    if one:
+        code = _data(what, mats)
+        if mats.dim() < 2 or not mats.is_contiguous():
+            raise ValueError(f"{what}: need a contiguous [..., m, n] tensor")
+        dev, (m, n) = mats.device, mats.shape[-2:]
+        if out is None:
+            out = _empty(stream, mats.shape, mats.dtype, dev)
+        else:
+            _dense(f"{what} out", out, mats.shape, mats.dtype, dev)
+        count = mats.numel() // (m * n) if m * n else 0
+        step = m * n * mats.element_size()
+        gp, op = ((_vp * count)(*[t.data_ptr() + i * step for i in range(count)]) for t in (mats, out))
+    else:
+        mats = list(mats)
+        if not mats:
+            return []
+        code = _data(what, mats[0])
+        dev = mats[0].device
+        if mats[0].dim() != 2:
+            raise ValueError(f"{what}: need [m, n] matrices")
+        (m, n), count = mats[0].shape, len(mats)
+        mats, gp = _matrices(what, mats)
+        out = [_empty(stream, t.shape, t.dtype, dev) for t in mats] if out is None else out
+        out, op = _matrices(f"{what} out", out, mats[0])
+        if len(out) != count:
+            raise ValueError(f"{what}: {len(out)} outputs for {count} matrices")
+    a = OrthoArgs(code, steps, count, m, n, *coeffs, eps, ctypes.cast(gp, _vp), ctypes.cast(op, _vp), None, 0)
+    _workspace(what, a, dev, stream)
+    _call(what, a, stream)
+    return out
+
+
+def fpde_muon_step(weights, grads, momenta, *, lr: float, momentum: float = 0.95, nesterov: bool = True,
+                   weight_decay: float = 0.0, scale: Optional[float] = None, steps: int = 5, coeffs=NS_COEFFS,
+                   eps: float = 1e-7, stream=None):
+    """Queue one Muon step of weight matrices of one shape, in place:
+
+        momentum <- mu momentum + grad;  u = grad + mu momentum (nesterov) or momentum
+        weight <- (1 - lr weight_decay) weight - lr scale orthogonalize(u)
+
+    ``weights`` and ``grads``: sequences of dense [m, n] tensors of one type, ``momenta``
+    float32 ones.  ``scale``: max(1, m / n)^(1/2) if None."""
+    what = "fpde_muon_step"
+    weights = list(weights)
+    if not weights:
+        return
+    code = _data(f"{what} weights", weights[0])
+    if weights[0].dim() != 2:
+        raise ValueError(f"{what}: need [m, n] matrices")
+    m, n = weights[0].shape
+    weights, wp = _matrices(f"{what} weights", weights)
+    grads, gp = _matrices(f"{what} grads", grads, weights[0])
+    momenta, mp = _matrices(f"{what} momenta", momenta, weights[0], torch.float32)
+    if len(grads) != len(weights) or len(momenta) != len(weights):
+        raise ValueError(f"{what}: {len(weights)} weights, {len(grads)} gradients, {len(momenta)} momenta")
+    if scale is None:
+        scale = max(1.0, m / max(1, n)) ** 0.5
+    a = MuonArgs(code, steps, bool(nesterov), 0, len(weights), m, n, *coeffs, eps, lr, momentum, weight_decay, scale,
+                 ctypes.cast(gp, _vp), ctypes.cast(mp, _vp), ctypes.cast(wp, _vp), None, 0)
+    _workspace(what, a, weights[0].device, stream)
+    _call(what, a, stream)
+
+
+class Muon(torch.optim.Optimizer):
+    """Muon over weight matrices: every step is one ``fpde_muon_step`` for each shape
+    and type among the parameters (all of them dense [m, n] CUDA matrices; biases,
+    norms and other vectors go to another optimiser)."""
+
+    def __init__(self, params, lr: float = 0.02, momentum: float = 0.95, nesterov: bool = True,
+                 weight_decay: float = 0.0, steps: int = 5, coeffs=NS_COEFFS, eps: float = 1e-7):
+        super().__init__(params, dict(lr=lr, momentum=momentum, nesterov=nesterov, weight_decay=weight_decay,
+                                      steps=steps, coeffs=tuple(coeffs), eps=eps))
+        for group in self.param_groups:
+            for p in group["params"]:
+                if p.dim() != 2:
+                    raise ValueError(f"Muon: parameters are matrices, got shape {tuple(p.shape)}")
+
+    @torch.no_grad()
+    def step(self, closure=None):
+        loss = None
+        if closure is not None:
+            with torch.enable_grad():
+                loss = closure()
+        for group in self.param_groups:
+            alike = {}
+            for p in group["params"]:
+                if p.grad is None:
+                    continue
+                state = self.state[p]
+                if "momentum" not in state:
+                    state["momentum"] = torch.zeros(p.shape, dtype=torch.float32, device=p.device)
+                alike.setdefault((p.shape, p.dtype), []).append(p)
+            for ps in alike.values():
+                fpde_muon_step(ps, [p.grad.contiguous() for p in ps], [self.state[p]["momentum"] for p in ps],
+                               lr=group["lr"], momentum=group["momentum"], nesterov=group["nesterov"],
+                               weight_decay=group["weight_decay"], steps=group["steps"], coeffs=group["coeffs"],
+                               eps=group["eps"])
+        return loss

@@ -98,3 +98,15 @@ def selective_scan(u, delta, A, B, C, D, z, bias, sp, state, lengths):
             y = y * silu(z[:, t])
         ys.append(torch.where(on[..., 0], y, torch.zeros((), dtype=y.dtype)))
     return (torch.stack(ys, 1) if ys else torch.zeros_like(u)), h
+
+
+def orthogonalize(g, steps, coeffs, eps):
+    """Newton-Schulz from the definition, from the side that is smaller."""
+    a, b, c = coeffs
+    x = g / (g.norm() + eps)
+    tall = g.shape[0] > g.shape[1]
+    x = x.t() if tall else x
+    for _ in range(steps):
+        k = x @ x.t()
+        x = a * x + (b * k + c * (k @ k)) @ x
+    return x.t() if tall else x
