@@ -4,28 +4,30 @@
 //   dp = dy (silu'(p) = q (1 + p (1 - q)), q = sigmoid(p));  dx_t = sum_k w_k dp_{t + W - 1 - k}
 //   dw_k = sum_t dp_t x_{t - W + 1 + k},  db = sum_t dp_t
 //
-// A lane owns the channels of one 16-byte load and marches a chunk of levels,
-// the last W - 1 of them in registers, so x is read once but for the W - 1 levels
-// before a chunk; the loads of kBlock levels are in flight together.  What bounds
-// both directions is memory.  The backward recomputes p from x instead of
-// reading it, and runs W - 1 levels past its chunk for the dp that dx needs there.
+// A lane owns 4 neighbouring channels and marches a chunk of levels, the last W - 1 of
+// them in registers, so x is read once but for the W - 1 levels before a chunk; the
+// next kBlock levels are on their way while those before them are worked on.  What
+// bounds both directions is memory: 4 channels (8 bytes of 16-bit data) a lane, not the
+// 8 of a 16-byte load, since the filters, windows and sums of 8 leave the backward one
+// wavefront a SIMD.  Where the channels are no multiple of 4 the last lane's four
+// begin earlier, and what two lanes own they write with the same values.  The backward
+// recomputes p from x instead of reading it, and runs W - 1 levels past its chunk for
+// the dp that dx needs there.
 #include "net_common.hpp"
 
 using namespace fpde_net;
 
 namespace {
 
-constexpr int kBlock = 8;    // levels whose loads are in flight together
-constexpr int kFwdChunk = 32;
-constexpr int kBwdChunk = 64;
+constexpr int kBlock = 8;  // levels whose loads are in flight together
 
 struct ConvP {
     const void *x, *dy, *w, *b, *state;
     const int32_t* lengths;
     void *y, *state_out;  // y: dx in the backward
-    float *dw, *db;       // partials [slots][channels * taps], [slots][channels]
+    float* part;          // [slots][channels * taps + channels]
     int64_t batch, chunks, xb, xt, dyb, dyt;
-    int length, channels, wf32, silu;
+    int length, channels, chunk, wf32, silu;
 };
 
 __device__ __forceinline__ int levels(const ConvP& P, int64_t b) {
@@ -37,12 +39,11 @@ __device__ __forceinline__ int levels(const ConvP& P, int64_t b) {
 // x at level t of sequence b, which holds len: its own levels, the carried state before
 // them, or zero
 template <class T, int W, int V>
-__device__ __forceinline__ void x_at(const ConvP& P, int64_t b, int t, int len, int c, int n,
-                                     float (&v)[V]) {
+__device__ __forceinline__ void x_at(const ConvP& P, int64_t b, int t, int len, int c, float (&v)[V]) {
     if (t >= 0 && t < len)
-        load_f32<T, V>(v, (const T*)P.x + b * P.xb + (int64_t)t * P.xt + c, n);
+        load_f32<T, V>(v, (const T*)P.x + b * P.xb + (int64_t)t * P.xt + c, V);
     else if (t < 0 && P.state)
-        load_f32<T, V>(v, (const T*)P.state + (b * (W - 1) + (W - 1 + t)) * P.channels + c, n);
+        load_f32<T, V>(v, (const T*)P.state + (b * (W - 1) + (W - 1 + t)) * P.channels + c, V);
     else {
 #pragma unroll
         for (int i = 0; i < V; ++i) v[i] = 0.f;
@@ -51,79 +52,96 @@ __device__ __forceinline__ void x_at(const ConvP& P, int64_t b, int t, int len, 
 
 // the filters of V channels: w[k][i], and the bias
 template <class T, int W, int V>
-__device__ __forceinline__ void load_filters(const ConvP& P, int c, int n, float (&w)[W][V], float (&b)[V]) {
+__device__ __forceinline__ void load_filters(const ConvP& P, int c, float (&w)[W][V], float (&b)[V]) {
+    float q[W * V];
+    load_param<T, W * V>(q, P.w, P.wf32, (int64_t)c * W, W * V);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
 #pragma unroll
-        for (int k = 0; k < W; ++k)
-            w[k][i] = i < n ? param<T>(P.w, P.wf32, (int64_t)(c + i) * W + k) : 0.f;
-        b[i] = P.b && i < n ? param<T>(P.b, P.wf32, c + i) : 0.f;
+        for (int k = 0; k < W; ++k) w[k][i] = q[i * W + k];
+        b[i] = 0.f;
+    }
+    if (P.b) load_param<T, V>(b, P.b, P.wf32, c, V);
+}
+
+// The first of a lane's V channels, or -1 past the last.
+template <int V>
+__device__ __forceinline__ int lane_channel(const ConvP& P) {
+    const int c = ((int)blockIdx.x * 64 + (int)threadIdx.x) * V;
+    return c >= P.channels ? -1 : (c < P.channels - V ? c : P.channels - V);
+}
+
+// kBlock levels from t on (clamped to the sequence's last, which exists)
+template <class T, int V>
+__device__ __forceinline__ void load_block(Raw<T, V> (&q)[kBlock], const void* x, int64_t b, int64_t bs, int64_t ts,
+                                           int t, int len, int c) {
+#pragma unroll
+    for (int j = 0; j < kBlock; ++j) {
+        const int s = t + j < len ? t + j : len - 1;
+        q[j] = load_raw<T, V>((const T*)x + b * bs + (int64_t)s * ts + c);
     }
 }
 
-template <class T, int W>
+template <class T, int W, int V>
 __global__ __launch_bounds__(64) void conv_fwd_kernel(ConvP P) {
-    constexpr int V = kVec<T>;
-    const int c = ((int)blockIdx.x * 64 + (int)threadIdx.x) * V, n = P.channels - c;
-    if (n <= 0) return;
+    const int c = lane_channel<V>(P);
+    if (c < 0) return;
     float w[W][V], bias[V];
-    load_filters<T, W, V>(P, c, n, w, bias);
+    load_filters<T, W, V>(P, c, w, bias);
     for (int64_t job = blockIdx.y; job < P.batch * P.chunks; job += gridDim.y) {
         const int64_t b = job / P.chunks;
-        const int t0 = (int)(job - b * P.chunks) * kFwdChunk, len = levels(P, b);
-        const int t1 = t0 + kFwdChunk < P.length ? t0 + kFwdChunk : P.length;
+        const int t0 = (int)(job - b * P.chunks) * P.chunk, len = levels(P, b);
+        const int t1 = t0 + P.chunk < P.length ? t0 + P.chunk : P.length, te = t1 < len ? t1 : len;
+        Raw<T, V> x[kBlock], nx[kBlock];
+        if (t0 < te) load_block<T, V>(x, P.x, b, P.xb, P.xt, t0, len, c);
         float win[W][V];  // win[k]: x at t - W + 1 + k
 #pragma unroll
-        for (int k = 0; k < W - 1; ++k) x_at<T, W, V>(P, b, t0 - (W - 1) + k, len, c, n, win[k + 1]);
+        for (int k = 0; k < W - 1; ++k) x_at<T, W, V>(P, b, t0 - (W - 1) + k, len, c, win[k + 1]);
         if (t0 == 0 && P.state_out) {
             // The lane that reads the state is the one that replaces it, after its reads.
             float last[W - 1][V];
 #pragma unroll
-            for (int i = 0; i < W - 1; ++i) x_at<T, W, V>(P, b, len - (W - 1) + i, len, c, n, last[i]);
+            for (int i = 0; i < W - 1; ++i) x_at<T, W, V>(P, b, len - (W - 1) + i, len, c, last[i]);
 #pragma unroll
             for (int i = 0; i < W - 1; ++i)
-                store_f32<T, V>((T*)P.state_out + (b * (W - 1) + i) * P.channels + c, last[i], n);
+                store_f32<T, V>((T*)P.state_out + (b * (W - 1) + i) * P.channels + c, last[i], V);
         }
-        T* y = (T*)P.y + (b * P.length + t0) * P.channels + c;
-        for (int t = t0; t < t1; t += kBlock) {
-            float x[kBlock][V];
-#pragma unroll
-            for (int j = 0; j < kBlock; ++j)
-                if (t + j < len && t + j < t1)
-                    load_f32<T, V>(x[j], (const T*)P.x + b * P.xb + (int64_t)(t + j) * P.xt + c, n);
+        T* y = (T*)P.y + (b * P.length) * P.channels + c;
+        for (int t = t0; t < te; t += kBlock) {
+            if (t + kBlock < te) load_block<T, V>(nx, P.x, b, P.xb, P.xt, t + kBlock, len, c);
 #pragma unroll
             for (int j = 0; j < kBlock; ++j) {
-                if (t + j >= t1) break;
-                float p[V];
+                if (t + j >= te) break;
+                float p[V], v[V];
+                unpack<T, V>(v, x[j]);
 #pragma unroll
-                for (int i = 0; i < V; ++i) p[i] = 0.f;
-                if (t + j < len) {
+                for (int i = 0; i < V; ++i) {
+                    p[i] = bias[i];
 #pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        p[i] = bias[i];
-#pragma unroll
-                        for (int k = 0; k < W - 1; ++k) {
-                            win[k][i] = win[k + 1][i];
-                            p[i] = fmaf(w[k][i], win[k][i], p[i]);
-                        }
-                        win[W - 1][i] = x[j][i];
-                        p[i] = fmaf(w[W - 1][i], x[j][i], p[i]);
-                        if (P.silu) p[i] = silu(p[i]);
+                    for (int k = 0; k < W - 1; ++k) {
+                        win[k][i] = win[k + 1][i];
+                        p[i] = fmaf(w[k][i], win[k][i], p[i]);
                     }
+                    win[W - 1][i] = v[i];
+                    p[i] = fmaf(w[W - 1][i], v[i], p[i]);
+                    if (P.silu) p[i] = silu(p[i]);
                 }
-                store_f32<T, V>(y + (int64_t)(t - t0 + j) * P.channels, p, n);
+                store_f32<T, V>(y + (int64_t)(t + j) * P.channels, p, V);
             }
+#pragma unroll
+            for (int j = 0; j < kBlock; ++j) x[j] = nx[j];
         }
+        const float zero[V] = {};
+        for (int t = te > t0 ? te : t0; t < t1; ++t) store_f32<T, V>(y + (int64_t)t * P.channels, zero, V);
     }
 }
 
-template <class T, int W>
+template <class T, int W, int V>
 __global__ __launch_bounds__(64) void conv_bwd_kernel(ConvP P) {
-    constexpr int V = kVec<T>;
-    const int c = ((int)blockIdx.x * 64 + (int)threadIdx.x) * V, n = P.channels - c;
-    if (n <= 0) return;
+    const int c = lane_channel<V>(P);
+    if (c < 0) return;
     float w[W][V], bias[V], dw[W][V], db[V];
-    load_filters<T, W, V>(P, c, n, w, bias);
+    load_filters<T, W, V>(P, c, w, bias);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         db[i] = 0.f;
@@ -132,32 +150,40 @@ __global__ __launch_bounds__(64) void conv_bwd_kernel(ConvP P) {
     }
     for (int64_t job = blockIdx.y; job < P.batch * P.chunks; job += gridDim.y) {
         const int64_t b = job / P.chunks;
-        const int t0 = (int)(job - b * P.chunks) * kBwdChunk, len = levels(P, b);
-        const int t1 = t0 + kBwdChunk < P.length ? t0 + kBwdChunk : P.length;
+        const int t0 = (int)(job - b * P.chunks) * P.chunk, len = levels(P, b);
+        const int t1 = t0 + P.chunk < P.length ? t0 + P.chunk : P.length;
+        // dx at level t - W + 1 is complete with dp at t: W - 1 levels more than the chunk has
+        const int tn = t1 + W - 1;
+        Raw<T, V> x[kBlock], g[kBlock], nx[kBlock], ng[kBlock];
+        if (t0 < len) {
+            load_block<T, V>(x, P.x, b, P.xb, P.xt, t0, len, c);
+            load_block<T, V>(g, P.dy, b, P.dyb, P.dyt, t0, len, c);
+        }
         float win[W][V];  // win[k]: x at t - W + 1 + k
         float dps[W][V];  // dps[k]: dp at t - W + 1 + k
 #pragma unroll
         for (int k = 0; k < W - 1; ++k) {
-            x_at<T, W, V>(P, b, t0 - (W - 1) + k, len, c, n, win[k + 1]);
+            x_at<T, W, V>(P, b, t0 - (W - 1) + k, len, c, win[k + 1]);
 #pragma unroll
             for (int i = 0; i < V; ++i) dps[k + 1][i] = 0.f;
         }
         T* dx = (T*)P.y + (b * P.length) * P.channels + c;
-        // dx at level t - W + 1 is complete with dp at t: W - 1 levels more than the chunk has
-        for (int t = t0; t < t1 + W - 1; t += kBlock) {
-            float x[kBlock][V], g[kBlock][V];
-#pragma unroll
-            for (int j = 0; j < kBlock; ++j)
-                if (t + j < len && t + j < t1 + W - 1) {
-                    load_f32<T, V>(x[j], (const T*)P.x + b * P.xb + (int64_t)(t + j) * P.xt + c, n);
-                    load_f32<T, V>(g[j], (const T*)P.dy + b * P.dyb + (int64_t)(t + j) * P.dyt + c, n);
-                }
+        for (int t = t0; t < tn; t += kBlock) {
+            if (t + kBlock < tn && t + kBlock < len) {
+                load_block<T, V>(nx, P.x, b, P.xb, P.xt, t + kBlock, len, c);
+                load_block<T, V>(ng, P.dy, b, P.dyb, P.dyt, t + kBlock, len, c);
+            }
 #pragma unroll
             for (int j = 0; j < kBlock; ++j) {
-                if (t + j >= t1 + W - 1) break;
+                if (t + j >= tn) break;
                 const bool own = t + j < t1;  // (the levels past the chunk count in the next one's dw)
-                float d[V];
+                float d[V], o[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) d[i] = 0.f;
                 if (t + j < len) {
+                    float v[V];
+                    unpack<T, V>(v, x[j]);
+                    unpack<T, V>(d, g[j]);
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
                         float p = bias[i];
@@ -166,23 +192,19 @@ __global__ __launch_bounds__(64) void conv_bwd_kernel(ConvP P) {
                             win[k][i] = win[k + 1][i];
                             p = fmaf(w[k][i], win[k][i], p);
                         }
-                        win[W - 1][i] = x[j][i];
-                        p = fmaf(w[W - 1][i], x[j][i], p);
-                        d[i] = g[j][i];
+                        win[W - 1][i] = v[i];
+                        p = fmaf(w[W - 1][i], v[i], p);
                         if (P.silu) {
                             const float q = sigmoid(p);
                             d[i] *= q * fmaf(p, 1.f - q, 1.f);
                         }
-                        const float o = own ? d[i] : 0.f;
-                        db[i] += o;
+                        if (own) {
+                            db[i] += d[i];
 #pragma unroll
-                        for (int k = 0; k < W; ++k) dw[k][i] = fmaf(o, win[k][i], dw[k][i]);
+                            for (int k = 0; k < W; ++k) dw[k][i] = fmaf(d[i], win[k][i], dw[k][i]);
+                        }
                     }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < V; ++i) d[i] = 0.f;
                 }
-                float o[V];
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     o[i] = 0.f;
@@ -199,19 +221,22 @@ __global__ __launch_bounds__(64) void conv_bwd_kernel(ConvP P) {
 #pragma unroll
                         for (int i = 0; i < V; ++i) o[i] = 0.f;
                     }
-                    store_f32<T, V>(dx + (int64_t)s * P.channels, o, n);
+                    store_f32<T, V>(dx + (int64_t)s * P.channels, o, V);
                 }
             }
+#pragma unroll
+            for (int j = 0; j < kBlock; ++j) x[j] = nx[j], g[j] = ng[j];
         }
     }
-    float* pw = P.dw + (int64_t)blockIdx.y * P.channels * W + (int64_t)c * W;
+    // a partial row: every channel's taps, then the biases
+    float* pw = P.part + (int64_t)blockIdx.y * P.channels * (W + 1);
+    float q[W * V];
 #pragma unroll
     for (int i = 0; i < V; ++i)
-        if (i < n) {
 #pragma unroll
-            for (int k = 0; k < W; ++k) pw[i * W + k] = dw[k][i];
-        }
-    if (P.db) store_f32<float, V>(P.db + (int64_t)blockIdx.y * P.channels + c, db, n);
+        for (int k = 0; k < W; ++k) q[i * W + k] = dw[k][i];
+    store_f32<float, W * V>(pw + (int64_t)c * W, q, W * V);
+    store_f32<float, V>(pw + (int64_t)P.channels * W + c, db, V);
 }
 
 // ---------------------------------------------------------------------------
@@ -220,7 +245,15 @@ __global__ __launch_bounds__(64) void conv_bwd_kernel(ConvP P) {
 constexpr int64_t kMaxChannels = 1 << 20, kMaxLevels = (int64_t)1 << 40;
 // Wavefronts of a launch before they loop over chunks.  The backward's partial
 // sums grow with them.
-constexpr int64_t kFwdWaves = 1 << 20, kBwdWaves = 8192;
+constexpr int64_t kFwdWaves = 1 << 20, kBwdWaves = 4096;
+
+// Levels of a chunk: 32, where the W - 1 levels read twice cost little, or 16 or 8 where
+// there would be fewer than one wavefront a SIMD.
+int chunk_of(int64_t batch, int64_t length, int64_t channels) {
+    int c = 32;
+    while (c > 8 && batch * cdiv(length, c) * cdiv(channels, 256) < 1024) c /= 2;
+    return c;
+}
 
 int check_conv(int dtype, int wdtype, int taps, int act, int64_t batch, int64_t length, int64_t channels) {
     if (size_of(dtype) == 0 || !(wdtype == FPDE_F32 || wdtype == dtype)) return FPDE_ERR_UNSUPPORTED;
@@ -240,20 +273,24 @@ bool strides_ok(int64_t bs, int64_t ts, int64_t batch, int64_t length, int64_t c
     return batch <= 1 || (bs >= 0 && bs <= most / batch);
 }
 
-int64_t slots(int64_t jobs, int64_t channels, int vec, int64_t waves) {
-    const int64_t n = waves / cdiv(channels, 64 * vec);
+int64_t slots(int64_t jobs, int64_t channels, int64_t waves) {
+    const int64_t n = waves / cdiv(channels, 256);
     const int64_t m = n < 1 ? 1 : (n > 65535 ? 65535 : n);
     return jobs < m ? (jobs < 1 ? 1 : jobs) : m;
 }
 
-// f(T{}, integral_constant<int, taps>)
+// f(T{}, integral_constant<int, taps>, integral_constant<int, channels a lane>): 4, or 1 where there
+// are fewer, or where lanes that share channels would read a state that the other replaces
 template <class F>
-int with_taps(int dtype, int taps, F f) {
+int with_taps(int dtype, int taps, bool one, F f) {
     return with_type(dtype, [&](auto t) {
+        auto v = [&](auto w) {
+            return one ? f(t, w, std::integral_constant<int, 1>{}) : f(t, w, std::integral_constant<int, 4>{});
+        };
         switch (taps) {
-        case 2: return f(t, std::integral_constant<int, 2>{});
-        case 3: return f(t, std::integral_constant<int, 3>{});
-        default: return f(t, std::integral_constant<int, 4>{});
+        case 2: return v(std::integral_constant<int, 2>{});
+        case 3: return v(std::integral_constant<int, 3>{});
+        default: return v(std::integral_constant<int, 4>{});
         }
     });
 }
@@ -286,12 +323,14 @@ extern "C" int fpde_causal_conv(const fpde_conv_args* a, void* stream) {
     P.batch = a->batch, P.xb = a->x_batch_stride, P.xt = a->x_time_stride;
     P.length = (int)a->length, P.channels = (int)a->channels;
     P.wf32 = a->weight_dtype == FPDE_F32, P.silu = a->silu;
-    P.chunks = a->length > 0 ? cdiv(a->length, kFwdChunk) : 1;
-    return with_taps(a->dtype, a->taps, [&](auto t, auto w) {
-        using T = decltype(t);
-        const dim3 g((unsigned)cdiv(a->channels, 64 * kVec<T>),
-                     (unsigned)slots(a->batch * P.chunks, a->channels, kVec<T>, kFwdWaves));
-        return launch(conv_fwd_kernel<T, decltype(w)::value>, g, dim3(64), (hipStream_t)stream, P);
+    P.chunk = chunk_of(a->batch, a->length, a->channels);
+    P.chunks = a->length > 0 ? cdiv(a->length, P.chunk) : 1;
+    const bool one = a->channels < 4 || (a->channels % 4 && a->state && a->state == a->state_out);
+    return with_taps(a->dtype, a->taps, one, [&](auto t, auto w, auto v) {
+        constexpr int V = decltype(v)::value;
+        const dim3 g((unsigned)cdiv(a->channels, 64 * V),
+                     (unsigned)slots(a->batch * P.chunks, a->channels, kFwdWaves));
+        return launch(conv_fwd_kernel<decltype(t), decltype(w)::value, V>, g, dim3(64), (hipStream_t)stream, P);
     });
 }
 
@@ -299,8 +338,8 @@ extern "C" int64_t fpde_causal_conv_bwd_workspace(const fpde_conv_bwd_args* a) {
     if (!a) return FPDE_ERR_ARG;
     const int st = check_conv(a->dtype, a->weight_dtype, a->taps, a->silu, a->batch, a->length, a->channels);
     if (st != FPDE_OK) return st;
-    const int64_t jobs = a->batch * cdiv(a->length, kBwdChunk);
-    return slots(jobs, a->channels, 16 / size_of(a->dtype), kBwdWaves) * a->channels * (a->taps + 1) * 4;
+    const int64_t jobs = a->batch * cdiv(a->length, chunk_of(a->batch, a->length, a->channels));
+    return slots(jobs, a->channels, kBwdWaves) * a->channels * (a->taps + 1) * 4;
 }
 
 extern "C" int fpde_causal_conv_bwd(const fpde_conv_bwd_args* a, void* stream) {
@@ -335,23 +374,19 @@ extern "C" int fpde_causal_conv_bwd(const fpde_conv_bwd_args* a, void* stream) {
     P.dyb = a->dy_batch_stride, P.dyt = a->dy_time_stride;
     P.length = (int)a->length, P.channels = (int)a->channels;
     P.wf32 = a->weight_dtype == FPDE_F32, P.silu = a->silu;
-    P.chunks = cdiv(a->length, kBwdChunk);
-    const int64_t jobs = a->batch * P.chunks;
-    const int64_t n = slots(jobs, a->channels, 16 / e, kBwdWaves), cols = a->channels * a->taps;
-    P.dw = (float*)a->workspace;
-    P.db = a->dbias ? P.dw + n * cols : nullptr;
+    P.chunk = chunk_of(a->batch, a->length, a->channels);
+    P.chunks = cdiv(a->length, P.chunk);
+    const int64_t jobs = a->batch * P.chunks, n = slots(jobs, a->channels, kBwdWaves);
+    P.part = (float*)a->workspace;
     hipStream_t s = (hipStream_t)stream;
     if (jobs > 0) {
-        st = with_taps(a->dtype, a->taps, [&](auto t, auto w) {
-            using T = decltype(t);
-            return launch(conv_bwd_kernel<T, decltype(w)::value>,
-                          dim3((unsigned)cdiv(a->channels, 64 * kVec<T>), (unsigned)n), dim3(64), s, P);
+        st = with_taps(a->dtype, a->taps, a->channels < 4, [&](auto t, auto w, auto v) {
+            constexpr int V = decltype(v)::value;
+            return launch(conv_bwd_kernel<decltype(t), decltype(w)::value, V>,
+                          dim3((unsigned)cdiv(a->channels, 64 * V), (unsigned)n), dim3(64), s, P);
         });
         if (st != FPDE_OK) return st;
     }
-    const int64_t rows = jobs > 0 ? n : 0;
-    st = queue_colsum(P.dw, rows, cols, cols, a->dweight, a->weight_dtype, s);
-    if (st == FPDE_OK && P.db)
-        st = queue_colsum(P.db, rows, a->channels, a->channels, a->dbias, a->weight_dtype, s);
-    return st;
+    return queue_colsum(P.part, jobs > 0 ? n : 0, a->channels * (a->taps + 1), a->dweight, a->channels * a->taps,
+                        a->dbias, a->dbias ? a->channels : 0, a->weight_dtype, s);
 }

@@ -47,7 +47,10 @@ __device__ __forceinline__ T from_f32(float v) {
 // V elements from p, of which the first n (> 0) exist; the others read as 0
 template <class T, int V>
 __device__ __forceinline__ void load_f32(float (&v)[V], const T* p, int n) {
-    if (n >= V) {
+    if constexpr (V == 1) {
+        v[0] = to_f32<T>(p[0]);
+        return;
+    } else if (n >= V) {
         const typename Pack<T, V>::type q = *(const typename Pack<T, V>::type*)p;
 #pragma unroll
         for (int i = 0; i < V; ++i) v[i] = to_f32<T>(q[i]);
@@ -59,7 +62,10 @@ __device__ __forceinline__ void load_f32(float (&v)[V], const T* p, int n) {
 
 template <class T, int V>
 __device__ __forceinline__ void store_f32(T* p, const float (&v)[V], int n) {
-    if (n >= V) {
+    if constexpr (V == 1) {
+        p[0] = from_f32<T>(v[0]);
+        return;
+    } else if (n >= V) {
         typename Pack<T, V>::type q;
 #pragma unroll
         for (int i = 0; i < V; ++i) q[i] = from_f32<T>(v[i]);
@@ -79,6 +85,24 @@ __device__ __forceinline__ void load_param(float (&v)[V], const void* p, bool f3
         load_f32<float, V>(v, (const float*)p + at, n);
     else
         load_f32<T, V>(v, (const T*)p + at, n);
+}
+
+// A vector as it lies in memory: loads of such are issued together, and nothing waits for
+// one of them before all are on their way.
+template <class T, int V>
+using Raw = typename Pack<T, V>::type;
+template <class T, int V>
+__device__ __forceinline__ Raw<T, V> load_raw(const T* p) {
+    return *(const Raw<T, V>*)p;
+}
+template <class T, int V>
+__device__ __forceinline__ void unpack(float (&v)[V], const Raw<T, V>& q) {
+    if constexpr (V == 1) {
+        v[0] = to_f32<T>(q);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = to_f32<T>(q[i]);
+    }
 }
 
 template <class T>
@@ -144,36 +168,41 @@ __device__ __forceinline__ float sigmoid(float x) {
 __device__ __forceinline__ float silu(float x) { return x * sigmoid(x); }
 
 // ---------------------------------------------------------------------------
-// Column sums of P partial rows of C floats each, in the order of the rows:
-// the second stage of every sum over rows, time levels or sequences.  A
-// workgroup owns 64 columns; its 16 wavefronts take every 16th row.
+// Column sums of partial rows of float32, `stride` apart, in a fixed order: the second
+// stage of every sum over rows, time levels or sequences.  Columns below `cols` go to
+// out, the `more` after them to out2.  A workgroup owns 32 columns; 32 groups of lanes
+// take every 32nd row, four rows in flight each, so that a few partial rows a lane are
+// one or two rounds of memory latency.
 template <class O>
 __global__ __launch_bounds__(1024) void colsum_kernel(const float* __restrict__ part, int64_t rows,
-                                                      int64_t cols, int64_t stride,
-                                                      O* __restrict__ out) {
-    __shared__ float red[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
-    float s = 0.f;
-    if (c < cols) {
-        const float* p = part + c;
-        int64_t r = wave;
-        float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
-        for (; r + 48 < rows; r += 64) {
-            s0 += p[r * stride];
-            s1 += p[(r + 16) * stride];
-            s2 += p[(r + 32) * stride];
-            s3 += p[(r + 48) * stride];
-        }
-        for (; r < rows; r += 16) s0 += p[r * stride];
-        s = (s0 + s1) + (s2 + s3);
-    }
-    red[wave][lane] = s;
-    __syncthreads();
-    if (wave == 0 && c < cols) {
+                                                      int64_t stride, O* __restrict__ out, int64_t cols,
+                                                      O* __restrict__ out2, int64_t more) {
+    __shared__ float red[32][33];
+    const int col = threadIdx.x & 31, grp = threadIdx.x >> 5;
+    const int64_t c = (int64_t)blockIdx.x * 32 + col;
+    const float* p = part + (c < cols + more ? c : 0);
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    int64_t r = grp;
+    for (; r + 96 < rows; r += 128) {
 #pragma unroll
-        for (int w = 1; w < 16; ++w) s += red[w][lane];
-        out[c] = from_f32<O>(s);
+        for (int i = 0; i < 4; ++i) s[i] += p[(r + 32 * i) * stride];
+    }
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        const float v = r + 32 * i < rows ? p[(r + 32 * i) * stride] : 0.f;
+        s[i] += v;
+    }
+    red[grp][col] = (s[0] + s[1]) + (s[2] + s[3]);
+    __syncthreads();
+    // group g adds the rows of column g
+    float v = red[col][grp];
+    v = lanes_reduce<32, AddOp>(v);
+    const int64_t w = (int64_t)blockIdx.x * 32 + grp;
+    if (col == 0) {
+        if (w < cols)
+            out[w] = from_f32<O>(v);
+        else if (w < cols + more)
+            out2[w - cols] = from_f32<O>(v);
     }
 }
 
@@ -201,14 +230,14 @@ inline int size_of(int dtype) {
     return dtype == FPDE_F32 ? 4 : dtype == FPDE_BF16 || dtype == FPDE_F16 ? 2 : 0;
 }
 
-inline int queue_colsum(const float* part, int64_t rows, int64_t cols, int64_t stride, void* out,
-                        int dtype, hipStream_t s) {
-    const dim3 g((unsigned)cdiv(cols, 64)), b(1024);
+inline int queue_colsum(const float* part, int64_t rows, int64_t stride, void* out, int64_t cols, void* out2,
+                        int64_t more, int dtype, hipStream_t s) {
+    const dim3 g((unsigned)cdiv(cols + more, 32)), b(1024);
     if (dtype == FPDE_F32)
-        return launch(colsum_kernel<float>, g, b, s, part, rows, cols, stride, (float*)out);
+        return launch(colsum_kernel<float>, g, b, s, part, rows, stride, (float*)out, cols, (float*)out2, more);
     if (dtype == FPDE_BF16)
-        return launch(colsum_kernel<bf16>, g, b, s, part, rows, cols, stride, (bf16*)out);
-    return launch(colsum_kernel<f16>, g, b, s, part, rows, cols, stride, (f16*)out);
+        return launch(colsum_kernel<bf16>, g, b, s, part, rows, stride, (bf16*)out, cols, (bf16*)out2, more);
+    return launch(colsum_kernel<f16>, g, b, s, part, rows, stride, (f16*)out, cols, (f16*)out2, more);
 }
 
 // f(T{}) for the element type of a dtype code that has been checked

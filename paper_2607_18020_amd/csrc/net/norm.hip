@@ -5,7 +5,11 @@
 // registers of LPR neighbouring lanes between the sum of its squares and its
 // output, so x and r are read once and y and s written once; what bounds it is
 // memory.  LPR grows with the width (16 lanes to a workgroup of 256) such that a
-// lane holds one or a few 16-byte loads: narrow rows share a wavefront.
+// lane holds one or a few 16-byte loads: narrow rows share a wavefront.  All loads
+// of a row are issued before the first is used, without a branch between them: a
+// lane past the row's end reads its first columns and counts them as 0, and where the
+// width is no multiple of a load the row's last load begins earlier and the columns
+// that it repeats count as 0.
 //
 // Backward: with rho = (mean(s^2) + eps)^-1/2 and g = w dy, differentiating
 // y_i = w_i s_i rho gives ds = dsum + rho g - rho^3 mean(g s) s.  Both row means
@@ -22,35 +26,42 @@ namespace {
 
 constexpr float kF8Max = 448.f, kF8Tiny = 0x1p-126f;
 
-// four float32 values, already in +-448 or NaN, as four e4m3 bytes
+// Four float32 values as four e4m3 bytes, rounded to nearest even.  Values divided by their
+// group's scale are at most 448 (1 + 2^-22), which rounds to 448; NaN, and what an infinite
+// scale makes of Inf, is NaN.
 __device__ __forceinline__ uint32_t pack_f8(float a, float b, float c, float d) {
     int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
     w = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
     return (uint32_t)w;
 }
 
-// y / sigma, held in +-448; a NaN stays one
-__device__ __forceinline__ float to_f8_range(float y, float sigma) {
-    const float q = y / sigma;
-    return q > kF8Max ? kF8Max : (q < -kF8Max ? -kF8Max : q);
-}
-
+// elements lo .. V - 1 of y / sigma as bytes from p on
 template <int V>
-__device__ __forceinline__ void store_f8(uint8_t* p, const float (&y)[V], float sigma, int n) {
+__device__ __forceinline__ void store_f8(uint8_t* p, const float (&y)[V], float sigma, int lo) {
     uint32_t w[V / 4];
+    const float inv = 1.f / sigma;  // (a product differs from the quotient by 2^-23, far below e4m3's step)
 #pragma unroll
     for (int i = 0; i < V / 4; ++i)
-        w[i] = pack_f8(to_f8_range(y[4 * i], sigma), to_f8_range(y[4 * i + 1], sigma),
-                       to_f8_range(y[4 * i + 2], sigma), to_f8_range(y[4 * i + 3], sigma));
-    if (n >= V) {
-        typedef uint32_t u32a1 __attribute__((aligned(1)));
-#pragma unroll
-        for (int i = 0; i < V / 4; ++i) ((u32a1*)p)[i] = w[i];
+        w[i] = pack_f8(y[4 * i] * inv, y[4 * i + 1] * inv, y[4 * i + 2] * inv, y[4 * i + 3] * inv);
+    if (lo == 0) {
+        typedef uint32_t words __attribute__((ext_vector_type(V / 4), aligned(1)));
+        if constexpr (V == 4)
+            *(typename Pack<uint8_t, 4>::type*)p = __builtin_bit_cast(typename Pack<uint8_t, 4>::type, w[0]);
+        else
+            *(words*)p = words{w[0], w[1]};
     } else {
 #pragma unroll
         for (int i = 0; i < V; ++i)
-            if (i < n) p[i] = (uint8_t)(w[i / 4] >> (8 * (i % 4)));
+            if (i >= lo) p[i] = (uint8_t)(w[i / 4] >> (8 * (i % 4)));
     }
+}
+
+template <int V>
+__device__ __forceinline__ void store_bytes(uint8_t* p, const float (&y)[V], float sigma, int lo) {
+    if constexpr (V == 1)
+        *p = (uint8_t)pack_f8(y[0] * (1.f / sigma), 0.f, 0.f, 0.f);
+    else
+        store_f8<V>(p, y, sigma, lo);
 }
 
 __device__ __forceinline__ float f8_scale(float amax) { return fmaxf(amax / kF8Max, kF8Tiny); }
@@ -68,33 +79,75 @@ struct NormP {
     float eps, inv_width;
 };
 
-// A row in LPR lanes x CH chunks of V columns; 256 threads.
-template <class T, bool F8, int LPR, int CH>
+// A lane's place in a row: the column of its first element of a chunk, and the first of its
+// V elements that counts (V: none).
+struct Cols {
+    int c, lo;
+};
+template <int V>
+__device__ __forceinline__ Cols cols_of(int c, int width) {
+    const int n = width - c;
+    return n >= V ? Cols{c, 0} : (n > 0 ? Cols{width - V, V - n} : Cols{0, V});
+}
+template <int V>
+__device__ __forceinline__ void mask(float (&v)[V], int lo) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = i >= lo ? v[i] : 0.f;
+}
+// elements lo .. V - 1
+template <class T, int V>
+__device__ __forceinline__ void store_from(T* p, const float (&v)[V], int lo) {
+    if (lo == 0) {
+        store_f32<T, V>(p, v, V);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i >= lo) p[i] = from_f32<T>(v[i]);
+    }
+}
+
+// A row in LPR lanes x CH chunks of V columns, V being 16 bytes of T, or 1 for rows narrower than
+// that; 256 threads.
+template <class T, bool F8, int V, int LPR, int CH>
 __global__ __launch_bounds__(256) void norm_fwd_kernel(NormP P) {
-    constexpr int V = kVec<T>, RPB = 256 / LPR;
+    constexpr int RPB = 256 / LPR;
     __shared__ float red[4];
-    const int lane = threadIdx.x % LPR;
-    for (int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / LPR;; row += (int64_t)gridDim.x * RPB) {
-        // (a workgroup's threads leave together where they meet at barriers: LPR = 256 is one row)
-        if (LPR == 256 ? row >= P.rows : row - threadIdx.x / LPR >= P.rows) break;
-        const bool live = row < P.rows;
-        float s[CH][V];
+    const int lane = threadIdx.x % LPR, sub = threadIdx.x / LPR;
+    for (int64_t row0 = (int64_t)blockIdx.x * RPB; row0 < P.rows; row0 += (int64_t)gridDim.x * RPB) {
+        const bool live = row0 + sub < P.rows;
+        const int64_t row = live ? row0 + sub : P.rows - 1;
+        Raw<T, V> xr[CH], rr[CH];
+        Cols at[CH];
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            at[k] = cols_of<V>((k * LPR + lane) * V, P.width);
+            xr[k] = load_raw<T, V>((const T*)P.x + row * P.xs + at[k].c);
+        }
+        if (P.r) {
+#pragma unroll
+            for (int k = 0; k < CH; ++k) rr[k] = load_raw<T, V>((const T*)P.r + row * P.rs + at[k].c);
+        }
+        float s[CH][V], w[CH][V];
+        if (P.w) {
+            if (P.wf32) {
+#pragma unroll
+                for (int k = 0; k < CH; ++k) load_f32<float, V>(w[k], (const float*)P.w + at[k].c, V);
+            } else {
+#pragma unroll
+                for (int k = 0; k < CH; ++k) load_f32<T, V>(w[k], (const T*)P.w + at[k].c, V);
+            }
+        }
         float ss = 0.f;
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
-            const int c = (k * LPR + lane) * V, n = live ? P.width - c : 0;
-            if (n > 0) {
-                load_f32<T, V>(s[k], (const T*)P.x + row * P.xs + c, n);
-                if (P.r) {
-                    float q[V];
-                    load_f32<T, V>(q, (const T*)P.r + row * P.rs + c, n);
+            unpack<T, V>(s[k], xr[k]);
+            if (P.r) {
+                float q[V];
+                unpack<T, V>(q, rr[k]);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) s[k][i] += q[i];
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < V; ++i) s[k][i] = 0.f;
+                for (int i = 0; i < V; ++i) s[k][i] += q[i];
             }
+            mask<V>(s[k], at[k].lo);
 #pragma unroll
             for (int i = 0; i < V; ++i) ss = fmaf(s[k][i], s[k][i], ss);
         }
@@ -103,43 +156,42 @@ __global__ __launch_bounds__(256) void norm_fwd_kernel(NormP P) {
         float rowmax = 0.f;
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
-            const int c = (k * LPR + lane) * V, n = live ? P.width - c : 0;
-            if (n > 0 && P.s) store_f32<T, V>((T*)P.s + row * P.width + c, s[k], n);
+            const int64_t e = row * P.width + at[k].c;
+            const bool put = live && at[k].lo < V;
+            if (put && P.s) store_from<T, V>((T*)P.s + e, s[k], at[k].lo);
 #pragma unroll
             for (int i = 0; i < V; ++i) s[k][i] *= rho;
-            if (n > 0 && P.w) {
-                float w[V];
-                load_param<T, V>(w, P.w, P.wf32, c, n);
+            if (P.w) {
+                // (elements that do not count may meet an Inf or NaN of a weight that is theirs elsewhere)
 #pragma unroll
-                for (int i = 0; i < V; ++i) s[k][i] *= w[i];
+                for (int i = 0; i < V; ++i) s[k][i] *= w[k][i];
             }
             if constexpr (F8) {
-                // a group of 128 columns is 128 / V neighbouring lanes of one chunk
+                // a group of 128 columns is 128 / V neighbouring lanes of one chunk (V = 1: the whole row)
                 float m = 0.f;
 #pragma unroll
-                for (int i = 0; i < V; ++i) m = fmaxf(m, n > i ? fabsf(s[k][i]) : 0.f);
+                for (int i = 0; i < V; ++i) m = fmaxf(m, i >= at[k].lo ? fabsf(s[k][i]) : 0.f);
                 if (P.group) {
-                    m = lanes_reduce<128 / V, MaxOp>(m);
-                    const float sigma = f8_scale(m);
-                    if (n > 0) {
-                        store_f8<V>((uint8_t*)P.y + row * P.width + c, s[k], sigma, n);
+                    const float sigma = f8_scale(lanes_reduce<(128 / V > LPR ? LPR : 128 / V), MaxOp>(m));
+                    const int c = (k * LPR + lane) * V;
+                    if (put) {
+                        store_bytes<V>((uint8_t*)P.y + e, s[k], sigma, at[k].lo);
                         if (c % 128 == 0) P.scales[row * P.ngroups + c / 128] = sigma;
                     }
                 } else {
                     rowmax = fmaxf(rowmax, m);
                 }
-            } else if (n > 0) {
-                store_f32<T, V>((T*)P.y + row * P.width + c, s[k], n);
+            } else if (put) {
+                store_from<T, V>((T*)P.y + e, s[k], at[k].lo);
             }
         }
         if constexpr (F8) {
             if (!P.group) {
                 const float sigma = f8_scale(group_reduce<LPR, MaxOp>(rowmax, red));
 #pragma unroll
-                for (int k = 0; k < CH; ++k) {
-                    const int c = (k * LPR + lane) * V, n = live ? P.width - c : 0;
-                    if (n > 0) store_f8<V>((uint8_t*)P.y + row * P.width + c, s[k], sigma, n);
-                }
+                for (int k = 0; k < CH; ++k)
+                    if (live && at[k].lo < V)
+                        store_bytes<V>((uint8_t*)P.y + row * P.width + at[k].c, s[k], sigma, at[k].lo);
                 if (live && lane == 0) P.scales[row] = sigma;
             }
         }
@@ -212,8 +264,16 @@ __global__ __launch_bounds__(1024) void norm_fwd_wide_kernel(NormP P) {
                 for (int i = 0; i < V; ++i) m = fmaxf(m, n > i ? fabsf(s[i]) : 0.f);
                 if (P.group) m = lanes_reduce<128 / V, MaxOp>(m);
                 const float sigma = f8_scale(P.group ? m : rowmax);
+                if (n >= V) {
+                    store_f8<V>((uint8_t*)P.y + row * P.width + c, s, sigma, 0);
+                } else if (n > 0) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const float one[1] = {s[i]};
+                        if (i < n) store_bytes<1>((uint8_t*)P.y + row * P.width + c + i, one, sigma, 0);
+                    }
+                }
                 if (n > 0) {
-                    store_f8<V>((uint8_t*)P.y + row * P.width + c, s, sigma, n);
                     if (P.group && c % 128 == 0) P.scales[row * P.ngroups + c / 128] = sigma;
                 }
             } else if (n > 0) {
@@ -233,38 +293,47 @@ struct NormBwdP {
     float eps, inv_width;
 };
 
-template <class T, int LPR, int CH>
+template <class T, int V, int LPR, int CH>
 __global__ __launch_bounds__(256) void norm_bwd_kernel(NormBwdP P) {
-    constexpr int V = kVec<T>, RPB = 256 / LPR;
+    constexpr int RPB = 256 / LPR;
     __shared__ float red[4], red2[4];
     __shared__ float acc[LPR == 256 ? 1 : RPB][LPR == 256 ? 1 : LPR * CH * V];
     const int lane = threadIdx.x % LPR, sub = threadIdx.x / LPR;
     float w[CH][V], dw[CH][V];
+    Cols at[CH];
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-        const int c = (k * LPR + lane) * V, n = P.width - c;
+        at[k] = cols_of<V>((k * LPR + lane) * V, P.width);
 #pragma unroll
         for (int i = 0; i < V; ++i) w[k][i] = 1.f, dw[k][i] = 0.f;
-        if (P.w && n > 0) load_param<T, V>(w[k], P.w, P.wf32, c, n);
+        if (P.w) load_param<T, V>(w[k], P.w, P.wf32, at[k].c, V);
     }
     for (int64_t row0 = (int64_t)blockIdx.x * RPB; row0 < P.rows; row0 += (int64_t)gridDim.x * RPB) {
-        const int64_t row = row0 + sub;
-        const bool live = row < P.rows;
+        const bool live = row0 + sub < P.rows;
+        const int64_t row = live ? row0 + sub : P.rows - 1;
+        Raw<T, V> sr[CH], gr[CH], dr[CH];
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            sr[k] = load_raw<T, V>((const T*)P.s + row * P.ss + at[k].c);
+            gr[k] = load_raw<T, V>((const T*)P.dy + row * P.dys + at[k].c);
+        }
+        if (P.dsum) {
+#pragma unroll
+            for (int k = 0; k < CH; ++k) dr[k] = load_raw<T, V>((const T*)P.dsum + row * P.dss + at[k].c);
+        }
         float s[CH][V], g[CH][V];
         float ss = 0.f, gs = 0.f;
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
-            const int c = (k * LPR + lane) * V, n = live ? P.width - c : 0;
-#pragma unroll
-            for (int i = 0; i < V; ++i) s[k][i] = 0.f, g[k][i] = 0.f;
-            if (n > 0) {
-                load_f32<T, V>(s[k], (const T*)P.s + row * P.ss + c, n);
-                load_f32<T, V>(g[k], (const T*)P.dy + row * P.dys + c, n);
-            }
+            const int lo = live ? at[k].lo : V;
+            unpack<T, V>(s[k], sr[k]);
+            unpack<T, V>(g[k], gr[k]);
+            mask<V>(s[k], lo);
+            mask<V>(g[k], lo);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 ss = fmaf(s[k][i], s[k][i], ss);
-                gs = fmaf(g[k][i] * w[k][i], s[k][i], gs);
+                gs = fmaf(i >= lo ? g[k][i] * w[k][i] : 0.f, s[k][i], gs);
             }
         }
         ss = group_reduce<LPR, AddOp>(ss, red);
@@ -273,35 +342,35 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(NormBwdP P) {
         const float c3 = rho * rho * rho * gs * P.inv_width;
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
-            const int c = (k * LPR + lane) * V, n = live ? P.width - c : 0;
-            if (n > 0) {
-                float d[V];
+            float d[V];
+            if (P.dsum) {
+                unpack<T, V>(d, dr[k]);
+            } else {
 #pragma unroll
                 for (int i = 0; i < V; ++i) d[i] = 0.f;
-                if (P.dsum) load_f32<T, V>(d, (const T*)P.dsum + row * P.dss + c, n);
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float t = rho * g[k][i];
-                    dw[k][i] = fmaf(t, s[k][i], dw[k][i]);
-                    d[i] += fmaf(t, w[k][i], -c3 * s[k][i]);
-                }
-                store_f32<T, V>((T*)P.ds + row * P.width + c, d, n);
             }
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float t = rho * g[k][i];
+                // (a row that does not exist has s = g = 0, but an eps of 0 leaves no rho)
+                dw[k][i] = live ? fmaf(t, s[k][i], dw[k][i]) : dw[k][i];
+                d[i] += fmaf(t, w[k][i], -c3 * s[k][i]);
+            }
+            if (live && at[k].lo < V) store_from<T, V>((T*)P.ds + row * P.width + at[k].c, d, at[k].lo);
         }
     }
     if (!P.part) return;
     float* out = P.part + (int64_t)blockIdx.x * P.width;
     if constexpr (LPR == 256) {
 #pragma unroll
-        for (int k = 0; k < CH; ++k) {
-            const int c = (k * LPR + lane) * V, n = P.width - c;
-            if (n > 0) store_f32<float, V>(out + c, dw[k], n);
-        }
+        for (int k = 0; k < CH; ++k)
+            if (at[k].lo < V) store_from<float, V>(out + at[k].c, dw[k], at[k].lo);
     } else {
 #pragma unroll
         for (int k = 0; k < CH; ++k)
 #pragma unroll
-            for (int i = 0; i < V; ++i) acc[sub][(k * LPR + lane) * V + i] = dw[k][i];
+            for (int i = 0; i < V; ++i)
+                if (i >= at[k].lo) acc[sub][at[k].c + i] = dw[k][i];
         __syncthreads();
         for (int c = threadIdx.x; c < P.width; c += 256) {
             float t = acc[0][c];
@@ -382,22 +451,30 @@ __global__ __launch_bounds__(256) void norm_dw_wide_kernel(NormBwdP P) {
 
 constexpr int64_t kMaxRows = (int64_t)1 << 40, kMaxWidth = 1 << 20;
 
-// lanes a row and 16-byte chunks a lane: f(LPR, CH) for the narrowest that holds the row;
-// f(0, 0) if none does
-template <class F>
-int with_layout(int64_t chunks, F f) {
-#define FPDE_L(L, C) f(std::integral_constant<int, L>{}, std::integral_constant<int, C>{})
-    if (chunks <= 16) return FPDE_L(16, 1);
-    if (chunks <= 32) return FPDE_L(32, 1);
-    if (chunks <= 64) return FPDE_L(64, 1);
-    if (chunks <= 128) return FPDE_L(64, 2);
-    if (chunks <= 256) return FPDE_L(64, 4);
-    if (chunks <= 512) return FPDE_L(256, 2);
-    if (chunks <= 1024) return FPDE_L(256, 4);
-    if (chunks <= 2048) return FPDE_L(256, 8);
-    return FPDE_L(0, 0);
+// Columns of a load, lanes a row and loads a lane: f(V, LPR, CH) for the smallest that holds the
+// row; f(0, 0, 0) if none does.  LEAST: the fewest lanes a row.
+template <class T, int LEAST, class F>
+int with_layout(int64_t width, F f) {
+    constexpr int V = kVec<T>, L16 = LEAST > 16 ? LEAST : 16;
+#define FPDE_L(W, L, C) \
+    f(std::integral_constant<int, W>{}, std::integral_constant<int, L>{}, std::integral_constant<int, C>{})
+    if (width < V) return FPDE_L(1, L16, 1);
+    const int64_t chunks = cdiv(width, V);
+    if (chunks <= L16) return FPDE_L(V, L16, 1);
+    if (chunks <= 32) return FPDE_L(V, 32, 1);
+    if (chunks <= 64) return FPDE_L(V, 64, 1);
+    if (chunks <= 128) return FPDE_L(V, 64, 2);
+    if (chunks <= 192) return FPDE_L(V, 64, 3);
+    if (chunks <= 256) return FPDE_L(V, 64, 4);
+    if (chunks <= 512) return FPDE_L(V, 256, 2);
+    if (chunks <= 768) return FPDE_L(V, 256, 3);
+    if (chunks <= 1024) return FPDE_L(V, 256, 4);
+    if (chunks <= 2048) return FPDE_L(V, 256, 8);
+    return FPDE_L(0, 0, 0);
 #undef FPDE_L
 }
+
+bool is_wide(int dtype, int64_t width) { return cdiv(width, 16 / size_of(dtype)) > 2048; }
 
 // Workgroups of the backward, which each write one partial row of dw: 4 for every
 // compute unit keep the loads in flight, and few partial rows keep their sum short.
@@ -461,22 +538,23 @@ extern "C" int fpde_rms_norm(const fpde_norm_args* a, void* stream) {
             (float)a->eps, (float)(1.0 / (double)a->width)};
     return with_type(a->dtype, [&](auto t) {
         using T = decltype(t);
-        return with_layout(cdiv(a->width, kVec<T>), [&](auto lpr, auto ch) {
-            constexpr int L = decltype(lpr)::value, C = decltype(ch)::value;
-            hipStream_t s = (hipStream_t)stream;
+        auto run = [&](auto f8c, auto v, auto lpr, auto ch) {
+            constexpr int V = decltype(v)::value, L = decltype(lpr)::value, C = decltype(ch)::value;
+            constexpr bool F8 = decltype(f8c)::value;
             if constexpr (L == 0) {
                 const dim3 g((unsigned)(a->rows < kMaxBlocks ? a->rows : kMaxBlocks));
-                return f8 ? launch(norm_fwd_wide_kernel<T, true>, g, dim3(1024), s, P)
-                          : launch(norm_fwd_wide_kernel<T, false>, g, dim3(1024), s, P);
+                return launch(norm_fwd_wide_kernel<T, F8>, g, dim3(1024), (hipStream_t)stream, P);
             } else {
-                // (8 bits in 16-lane rows of float32: a group of 128 columns needs 32 lanes)
-                constexpr int L8 = L < 128 / kVec<T> ? 128 / kVec<T> : L;
-                const int64_t n = cdiv(a->rows, f8 ? 256 / L8 : 256 / L);
+                const int64_t n = cdiv(a->rows, 256 / L);
                 const dim3 g((unsigned)(n < kMaxBlocks ? n : kMaxBlocks));
-                return f8 ? launch(norm_fwd_kernel<T, true, L8, C>, g, dim3(256), s, P)
-                          : launch(norm_fwd_kernel<T, false, L, C>, g, dim3(256), s, P);
+                return launch(norm_fwd_kernel<T, F8, V, L, C>, g, dim3(256), (hipStream_t)stream, P);
             }
-        });
+        };
+        if (!f8)
+            return with_layout<T, 1>(a->width, [&](auto v, auto l, auto c) { return run(std::false_type{}, v, l, c); });
+        // (8 bits: a group of 128 columns has to lie in one row's lanes)
+        return with_layout<T, 128 / kVec<T>>(a->width,
+                                             [&](auto v, auto l, auto c) { return run(std::true_type{}, v, l, c); });
     });
 }
 
@@ -485,8 +563,7 @@ extern "C" int64_t fpde_rms_norm_bwd_workspace(const fpde_norm_bwd_args* a) {
     const int st = check_norm(a->dtype, a->weight_dtype, a->rows, a->width, a->eps);
     if (st != FPDE_OK) return st;
     if (!a->dweight) return 0;
-    const int64_t chunks = cdiv(a->width, 16 / size_of(a->dtype));
-    return with_layout(chunks, [&](auto lpr, auto) { return (int)decltype(lpr)::value; }) == 0
+    return is_wide(a->dtype, a->width)
                ? (kWideGroups * a->width + a->rows) * 4
                : kBwdBlocks * a->width * 4;
 }
@@ -517,12 +594,12 @@ extern "C" int fpde_rms_norm_bwd(const fpde_norm_bwd_args* a, void* stream) {
                nullptr, a->rows, a->dy_stride, a->sum_stride, a->dsum_stride, (int)a->width,
                a->weight_dtype == FPDE_F32, (float)a->eps, (float)(1.0 / (double)a->width)};
     if (a->rows == 0)
-        return a->dweight ? queue_colsum(P.part, 0, a->width, a->width, a->dweight, a->weight_dtype, s)
+        return a->dweight ? queue_colsum(P.part, 0, a->width, a->dweight, a->width, nullptr, 0, a->weight_dtype, s)
                           : FPDE_OK;
     return with_type(a->dtype, [&](auto t) {
         using T = decltype(t);
-        return with_layout(cdiv(a->width, kVec<T>), [&](auto lpr, auto ch) {
-            constexpr int L = decltype(lpr)::value, C = decltype(ch)::value;
+        return with_layout<T, 1>(a->width, [&](auto v, auto lpr, auto ch) {
+            constexpr int V = decltype(v)::value, L = decltype(lpr)::value, C = decltype(ch)::value;
             int64_t parts;
             int r;
             if constexpr (L == 0) {
@@ -543,10 +620,10 @@ extern "C" int fpde_rms_norm_bwd(const fpde_norm_bwd_args* a, void* stream) {
                 if (r == FPDE_OK && P.part && !first) r = queue_dw_wide<T>(P, parts, s);
             } else {
                 parts = bwd_blocks(a->rows, 256 / L);
-                r = launch(norm_bwd_kernel<T, L, C>, dim3((unsigned)parts), dim3(256), s, P);
+                r = launch(norm_bwd_kernel<T, V, L, C>, dim3((unsigned)parts), dim3(256), s, P);
             }
             if (r != FPDE_OK || !P.part) return r;
-            return queue_colsum(P.part, parts, a->width, a->width, a->dweight, a->weight_dtype, s);
+            return queue_colsum(P.part, parts, a->width, a->dweight, a->width, nullptr, 0, a->weight_dtype, s);
         });
     });
 }

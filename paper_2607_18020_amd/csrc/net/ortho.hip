@@ -61,23 +61,24 @@ struct Mats {
     float eps;
 };
 
-// u of element i, the momentum brought up to date (update) or read as it is now
-template <class T>
-__device__ __forceinline__ float update_of(const Mats& M, int mat, int64_t i, bool update) {
-    const float g = to_f32<T>(((const T*)M.g[mat])[i]);
-    if (!M.muon) return g;
-    float m = M.mom[mat][i];
-    if (update) {
-        m = fmaf(M.mu, m, g);
-        M.mom[mat][i] = m;
-    }
-    return M.nesterov ? fmaf(M.mu, m, g) : m;
+// u from a gradient and a momentum that is up to date
+__device__ __forceinline__ float update_of(const Mats& M, float g, float m) {
+    return !M.muon ? g : (M.nesterov ? fmaf(M.mu, m, g) : m);
 }
 
+// the first k of 8 neighbouring elements from i on: results, or weights
 template <class T>
-__device__ __forceinline__ void finish(const Mats& M, int mat, int64_t i, float x) {
+__device__ __forceinline__ void finish(const Mats& M, int mat, int64_t i, const float (&x)[8], int k) {
     T* o = (T*)M.out[mat] + i;
-    *o = from_f32<T>(M.muon ? fmaf(M.keep, to_f32<T>(*o), -M.rate * x) : x);
+    if (M.muon) {
+        float w[8];
+        load_f32<T, 8>(w, o, k);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = fmaf(M.keep, w[e], -M.rate * x[e]);
+        store_f32<T, 8>(o, w, k);
+    } else {
+        store_f32<T, 8>(o, x, k);
+    }
 }
 
 __device__ __forceinline__ double wave_sum(double v) {
@@ -117,14 +118,15 @@ __device__ __forceinline__ void lds_product(f32x4 (&acc)[MT][NT], const f16* U, 
             vh[j] = *(const f16x8*)(V + (j * 16 + r) * pv + k);
             vl[j] = *(const f16x8*)(V + hv + (j * 16 + r) * pv + k);
         }
+        // (a sum's three products are apart, so that none waits for the one before)
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+        for (int p = 0; p < 3; ++p)
 #pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(uh[i], vl[j], acc[i][j], 0, 0, 0);
-                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ul[i], vh[j], acc[i][j], 0, 0, 0);
-                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(uh[i], vh[j], acc[i][j], 0, 0, 0);
-            }
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p == 1 ? ul[i] : uh[i], p ? vh[j] : vl[j],
+                                                                       acc[i][j], 0, 0, 0);
     }
 }
 
@@ -162,16 +164,35 @@ __global__ __launch_bounds__(512) void ortho_small_kernel(Mats M, int steps, flo
     };
     float x[MT][NT][4];
     double ss = 0.0;
+    // Elements past the matrix repeat its last ones and then count as 0: no load waits for a branch.
+    auto each = [&](auto f) {
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+        for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
+            for (int j = 0; j < NT; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int row = row0 + i * 16 + r4 + e, col = col0 + j * 16 + cl;
-                x[i][j][e] = row < s && col < l ? update_of<T>(M, mat, index(row, col), true) : 0.f;
-                ss += (double)x[i][j][e] * (double)x[i][j][e];
+                for (int e = 0; e < 4; ++e) {
+                    const int row = row0 + i * 16 + r4 + e, col = col0 + j * 16 + cl;
+                    const bool in = row < s && col < l;
+                    f(i, j, e, index(row < s ? row : s - 1, col < l ? col : l - 1), in);
+                }
+    };
+    {
+        T g[MT][NT][4];
+        each([&](int i, int j, int e, int64_t k, bool) { g[i][j][e] = ((const T*)M.g[mat])[k]; });
+        if (M.muon)
+            each([&](int i, int j, int e, int64_t k, bool) { x[i][j][e] = M.mom[mat][k]; });
+        each([&](int i, int j, int e, int64_t k, bool in) {
+            float v = to_f32<T>(g[i][j][e]);
+            if (M.muon) {
+                const float m = fmaf(M.mu, x[i][j][e], v);
+                if (in) M.mom[mat][k] = m;
+                v = update_of(M, v, m);
             }
+            x[i][j][e] = in ? v : 0.f;
+            ss += (double)x[i][j][e] * (double)x[i][j][e];
+        });
+    }
     ss = wave_sum(ss);
     if (lane == 0) sums[wave] = ss;
     __syncthreads();
@@ -237,21 +258,18 @@ __global__ __launch_bounds__(512) void ortho_small_kernel(Mats M, int steps, flo
                 for (int e = 0; e < 4; ++e) x[i][j][e] = fmaf(ca, x[i][j][e], y[i][j][e] * kInvSS);
         __syncthreads();
     }
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int row = row0 + i * 16 + r4 + e, col = col0 + j * 16 + cl;
-                if (row < s && col < l) finish<T>(M, mat, index(row, col), x[i][j][e]);
-            }
+    T w[MT][NT][4];
+    if (M.muon) each([&](int i, int j, int e, int64_t k, bool) { w[i][j][e] = ((const T*)M.out[mat])[k]; });
+    each([&](int i, int j, int e, int64_t k, bool in) {
+        const float v = M.muon ? fmaf(M.keep, to_f32<T>(w[i][j][e]), -M.rate * x[i][j][e]) : x[i][j][e];
+        if (in) ((T*)M.out[mat])[k] = from_f32<T>(v);
+    });
 }
 
 // ---------------------------------------------------------------------------
 // Large matrices.
 
-constexpr int kNormBlocks = 256;  // partial sums of squares a matrix
+constexpr int kNormBlocks = 1024;  // partial sums of squares a matrix
 
 template <class T>
 __global__ __launch_bounds__(256) void ortho_norm_kernel(Mats M, double* part) {
@@ -259,9 +277,21 @@ __global__ __launch_bounds__(256) void ortho_norm_kernel(Mats M, double* part) {
     const int mat = (int)blockIdx.y;
     const int64_t n = (int64_t)M.m * M.n;
     double ss = 0.0;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)kNormBlocks * 256) {
-        const float v = update_of<T>(M, mat, i, true);
-        ss += (double)v * (double)v;
+    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < n; i += (int64_t)kNormBlocks * 1024) {
+        const int k = n - i < 4 ? (int)(n - i) : 4;
+        float v[4], m[4];
+        load_f32<T, 4>(v, (const T*)M.g[mat] + i, k);
+        if (M.muon) {
+            load_f32<float, 4>(m, M.mom[mat] + i, k);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                m[e] = fmaf(M.mu, m[e], v[e]);
+                v[e] = update_of(M, v[e], m[e]);
+            }
+            store_f32<float, 4>(M.mom[mat] + i, m, k);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) ss += (double)v[e] * (double)v[e];
     }
     ss = wave_sum(ss);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = ss;
@@ -282,24 +312,30 @@ __global__ __launch_bounds__(256) void ortho_split_kernel(Mats M, const double* 
     __shared__ float tile[64][65];
     __shared__ double red[4];
     const int mat = (int)blockIdx.z, lane = (int)(threadIdx.x & 63), wave = (int)(threadIdx.x >> 6);
-    double ss = wave_sum(part[mat * kNormBlocks + threadIdx.x]);
+    const double* q = part + mat * kNormBlocks + threadIdx.x;
+    double ss = wave_sum((q[0] + q[256]) + (q[512] + q[768]));
     if (lane == 0) red[wave] = ss;
     __syncthreads();
     ss = (red[0] + red[1]) + (red[2] + red[3]);
     const float inv = inv_norm(ss, M.eps);
     const int r0 = (int)blockIdx.y * 64, c0 = (int)blockIdx.x * 64;
     const int s = M.tall ? M.n : M.m, l = M.tall ? M.m : M.n;
-    for (int i = wave; i < 64; i += 4) {
-        // neighbouring lanes read neighbouring elements of the stored matrix
-        const int row = M.tall ? r0 + lane : r0 + i, col = M.tall ? c0 + i : c0 + lane;
-        float v = 0.f;
-        if (row < s && col < l)
-            v = inv * update_of<T>(M, mat, M.tall ? (int64_t)col * M.n + row : (int64_t)row * M.n + col, false);
-        if (M.tall)
-            tile[lane][i] = v;
-        else
-            tile[i][lane] = v;
-    }
+    float g[16], m[16];
+    auto each = [&](auto f) {
+#pragma unroll
+        for (int h = 0; h < 16; ++h) {
+            // neighbouring lanes read neighbouring elements of the stored matrix; those past it
+            // repeat its last ones and count as 0
+            const int i = wave + h * 4, row = M.tall ? r0 + lane : r0 + i, col = M.tall ? c0 + i : c0 + lane;
+            const int rr = row < s ? row : s - 1, cc = col < l ? col : l - 1;
+            f(h, i, M.tall ? (int64_t)cc * M.n + rr : (int64_t)rr * M.n + cc, row < s && col < l);
+        }
+    };
+    each([&](int h, int, int64_t k, bool) { g[h] = to_f32<T>(((const T*)M.g[mat])[k]); });
+    if (M.muon) each([&](int h, int, int64_t k, bool) { m[h] = M.mom[mat][k]; });
+    each([&](int h, int i, int64_t, bool in) {
+        (M.tall ? tile[lane][i] : tile[i][lane]) = in ? inv * update_of(M, g[h], m[h]) : 0.f;
+    });
     __syncthreads();
     for (int i = wave; i < 64; i += 4) {
         const int64_t a = mat * X.step + (int64_t)(r0 + i) * X.ld + c0 + lane;
@@ -332,8 +368,11 @@ __global__ __launch_bounds__(256) void ortho_product_kernel(Prod P, Mats M) {
     constexpr int CH = TILE * 4;                       // 16-byte chunks of a TILE x 32 operand tile
     constexpr int W = TILE / 2, F = W / 32;            // a wavefront's share, in 32 x 32 tiles
     constexpr int STAGE = 4 * CH;                      // chunks: U hi, U lo, V hi, V lo
-    constexpr int OUT = TILE * (TILE + 1) * 4;         // the result tile in float32
-    constexpr int BYTES = 2 * STAGE * 16 > OUT ? 2 * STAGE * 16 : OUT;
+    constexpr int NB = TILE == 64 ? 4 : 2;             // operand tiles in LDS, NB - 1 of them on their way
+    constexpr int LOADS = 4 * CH / 256;                // a wavefront's loads a tile
+    constexpr int PT = TILE + 4;                       // the result tile in float32: its pitch
+    constexpr int OUT = TILE * PT * 4;
+    constexpr int BYTES = NB * STAGE * 16 > OUT ? NB * STAGE * 16 : OUT;
     __shared__ __attribute__((aligned(16))) char lds[BYTES];
     const int mat = (int)blockIdx.y, lane = (int)(threadIdx.x & 63);
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -363,19 +402,30 @@ __global__ __launch_bounds__(256) void ortho_product_kernel(Prod P, Mats M) {
     auto operand = [&](int o, int buf, int row, int ch) {
         return *(const f16x8*)(lds + ((buf * 4 + o) * CH + row * 4 + (ch ^ ((row >> 2) & 3))) * 16);
     };
-    f32x16 acc[F][F];
+    // A sum's three products in turn would each wait for the one before: with four tiles a wavefront
+    // they are four instructions apart, with one tile each has a sum of its own.
+    constexpr int S = F == 1 ? 3 : 1;
+    f32x16 acc[S][F][F];
 #pragma unroll
-    for (int i = 0; i < F; ++i)
+    for (int p = 0; p < S; ++p)
 #pragma unroll
-        for (int j = 0; j < F; ++j)
+        for (int i = 0; i < F; ++i)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-    fetch(0, 0);
+            for (int j = 0; j < F; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[p][i][j][e] = 0.f;
+#pragma unroll
+    for (int i = 0; i < NB - 1; ++i)
+        if (i * 32 < P.K) fetch(i * 32, i);
     int buf = 0;
-    for (int k = 0; k < P.K; k += 32, buf ^= 1) {
-        __builtin_amdgcn_s_waitcnt(0);  // this wavefront's part of the tile is in LDS
-        __syncthreads();                // everyone's is, and nobody reads the other buffer any more
-        if (k + 32 < P.K) fetch(k + 32, buf ^ 1);
+    for (int k = 0; k < P.K; k += 32, buf = buf + 1 == NB ? 0 : buf + 1) {
+        // This wavefront's part of the tile is in LDS when all but the later tiles' loads have arrived;
+        // past the barrier everyone's is, and nobody reads the tile before any more.
+        if (k + (NB - 2) * 32 < P.K)
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((NB - 2) * LOADS) : "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (k + (NB - 1) * 32 < P.K) fetch(k + (NB - 1) * 32, buf == 0 ? NB - 1 : buf - 1);
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
             f16x8 uh[F], ul[F], vh[F], vl[F];
@@ -387,57 +437,93 @@ __global__ __launch_bounds__(256) void ortho_product_kernel(Prod P, Mats M) {
                 vl[i] = operand(3, buf, wc + i * 32 + r, kk * 2 + kh);
             }
 #pragma unroll
-            for (int i = 0; i < F; ++i)
+            for (int p = 0; p < 3; ++p)
 #pragma unroll
-                for (int j = 0; j < F; ++j) {
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(uh[i], vl[j], acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ul[i], vh[j], acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(uh[i], vh[j], acc[i][j], 0, 0, 0);
-                }
+                for (int i = 0; i < F; ++i)
+#pragma unroll
+                    for (int j = 0; j < F; ++j)
+                        acc[p % S][i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                            p == 1 ? ul[i] : uh[i], p ? vh[j] : vl[j], acc[p % S][i][j], 0, 0, 0);
         }
     }
-    // The tile by way of LDS, so that both orders are written along their rows.
+    // The tile by way of LDS, so that both orders are written along their rows, 8 elements a lane.
+    constexpr int IT = TILE * TILE / 8 / 256;
+    f16x8 zh[IT], zl[IT];
+    auto spot = [&](int it, int* row, int* col) {
+        const int q = it * 256 + (int)threadIdx.x;
+        *row = q / (TILE / 8), *col = q % (TILE / 8) * 8;
+    };
+    if (P.Z.hi) {
+#pragma unroll
+        for (int it = 0; it < IT; ++it) {
+            int row, col;
+            spot(it, &row, &col);
+            const int64_t z = mat * P.Z.step + (int64_t)(tr * TILE + row) * P.Z.ld + tc * TILE + col;
+            zh[it] = *(const f16x8*)(P.Z.hi + z);
+            zl[it] = *(const f16x8*)(P.Z.lo + z);
+        }
+    }
     __syncthreads();
     float* t = (float*)lds;
-    constexpr int PT = TILE + 1;
 #pragma unroll
     for (int i = 0; i < F; ++i)
 #pragma unroll
         for (int j = 0; j < F; ++j)
 #pragma unroll
-            for (int e = 0; e < 16; ++e)
-                t[(wr + i * 32 + (e & 3) + 8 * (e >> 2) + 4 * kh) * PT + wc + j * 32 + r] = acc[i][j][e] * P.cp;
-    __syncthreads();
-    for (int q = (int)threadIdx.x; q < TILE * TILE; q += 256) {
-        const int row = q / TILE, col = q % TILE;
-        float v = t[row * PT + col];
-        if (P.Z.hi) {
-            const int64_t z = mat * P.Z.step + (int64_t)(tr * TILE + row) * P.Z.ld + tc * TILE + col;
-            v = fmaf(P.ca * kInvS, (float)P.Z.hi[z] + (float)P.Z.lo[z], v);
-        }
-        if constexpr (LAST) {
-            if (M.tall) {
-                t[row * PT + col] = v;
-            } else if (tr * TILE + row < M.m && tc * TILE + col < M.n) {
-                finish<T>(M, mat, (int64_t)(tr * TILE + row) * M.n + tc * TILE + col, v);
+            for (int e = 0; e < 16; ++e) {
+                float v = acc[0][i][j][e];
+                if (S == 3) v += acc[1 % S][i][j][e] + acc[2 % S][i][j][e];
+                t[(wr + i * 32 + (e & 3) + 8 * (e >> 2) + 4 * kh) * PT + wc + j * 32 + r] = v * P.cp;
             }
+    __syncthreads();
+    auto put = [&](const Half& H, int row, int col, const float (&v)[8]) {
+        f16x8 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            f16 a, b;
+            split(v[e], a, b);
+            hi[e] = a, lo[e] = b;
+        }
+        const int64_t c = mat * H.step + (int64_t)row * H.ld + col;
+        *(f16x8*)(H.hi + c) = hi;
+        *(f16x8*)(H.lo + c) = lo;
+    };
+    const bool both = LAST ? M.tall : !(P.sym && tr == tc);
+#pragma unroll
+    for (int it = 0; it < IT; ++it) {
+        int row, col;
+        spot(it, &row, &col);
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            v[e] = t[row * PT + col + e];
+            if (P.Z.hi) v[e] = fmaf(P.ca * kInvS, (float)zh[it][e] + (float)zl[it][e], v[e]);
+        }
+        if (both) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) t[row * PT + col + e] = v[e];
+        }
+        const int grow = tr * TILE + row, gcol = tc * TILE + col;
+        if constexpr (LAST) {
+            if (!M.tall && grow < M.m && gcol < M.n) finish<T>(M, mat, (int64_t)grow * M.n + gcol, v, M.n - gcol);
         } else {
-            const int64_t c = mat * P.C.step + (int64_t)(tr * TILE + row) * P.C.ld + tc * TILE + col;
-            split(v, P.C.hi[c], P.C.lo[c]);
-            t[row * PT + col] = v;
+            put(P.C, grow, gcol, v);
         }
     }
-    if (LAST ? !M.tall : (P.sym && tr == tc)) return;
+    if (!both) return;
     __syncthreads();
-    for (int q = (int)threadIdx.x; q < TILE * TILE; q += 256) {
-        const int col = q / TILE, row = q % TILE;
-        const float v = t[row * PT + col];
+#pragma unroll
+    for (int it = 0; it < IT; ++it) {
+        // 16 neighbouring columns and 4 groups of rows a wavefront: few lanes meet in a bank
+        const int q = it * 256 + (int)threadIdx.x, col = q % 16 + q / (16 * (TILE / 8)) * 16;
+        const int row = q / 16 % (TILE / 8) * 8, grow = tr * TILE + row, gcol = tc * TILE + col;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = t[(row + e) * PT + col];
         if constexpr (LAST) {
-            if (tc * TILE + col < M.m && tr * TILE + row < M.n)
-                finish<T>(M, mat, (int64_t)(tc * TILE + col) * M.n + tr * TILE + row, v);
+            if (gcol < M.m && grow < M.n) finish<T>(M, mat, (int64_t)gcol * M.n + grow, v, M.n - grow);
         } else {
-            const int64_t c = mat * P.Ct.step + (int64_t)(tc * TILE + col) * P.Ct.ld + tr * TILE + row;
-            split(v, P.Ct.hi[c], P.Ct.lo[c]);
+            put(P.Ct, gcol, grow, v);
         }
     }
 }

@@ -815,9 +815,10 @@ extern "C" int fpde_selective_scan_bwd(const fpde_scan_bwd_args* a, void* stream
         if (st != FPDE_OK) return st;
     }
     const int64_t rows = n > 0 ? p.slots : 0, cols = a->channels * a->states;
-    st = queue_colsum(P.pA, rows, cols, cols, a->dA, FPDE_F32, s);
-    if (st == FPDE_OK && P.pD) st = queue_colsum(P.pD, rows, a->channels, a->channels, a->dD, FPDE_F32, s);
+    st = queue_colsum(P.pA, rows, cols, a->dA, cols, nullptr, 0, FPDE_F32, s);
+    if (st == FPDE_OK && P.pD)
+        st = queue_colsum(P.pD, rows, a->channels, a->dD, a->channels, nullptr, 0, FPDE_F32, s);
     if (st == FPDE_OK && P.pbias)
-        st = queue_colsum(P.pbias, rows, a->channels, a->channels, a->ddelta_bias, FPDE_F32, s);
+        st = queue_colsum(P.pbias, rows, a->channels, a->ddelta_bias, a->channels, nullptr, 0, FPDE_F32, s);
     return st;
 }

@@ -101,6 +101,7 @@ CALLS = {"fpde_rms_norm": (NormArgs, False), "fpde_rms_norm_bwd": (NormBwdArgs, 
 EXPORTED = tuple(CALLS) + tuple(n + "_workspace" for n, (_, ws) in CALLS.items() if ws)
 
 _lib = None
+_fns = {}  # entry points by name, once the library is loaded
 
 
 def _load():
@@ -112,9 +113,11 @@ def _load():
         for name, (args, ws) in CALLS.items():
             fn = getattr(lib_, name)
             fn.argtypes, fn.restype = [ctypes.POINTER(args), _vp], ctypes.c_int
+            _fns[name] = fn
             if ws:
                 fn = getattr(lib_, name + "_workspace")
                 fn.argtypes, fn.restype = [ctypes.POINTER(args)], _i64
+                _fns[name + "_workspace"] = fn
         _lib = lib_
     return _lib
 
@@ -124,15 +127,21 @@ def lib():
     return _load()
 
 
+def _fn(name):
+    if _lib is None:
+        _load()
+    return _fns[name]
+
+
 def _call(name, args, stream):
-    st = getattr(_lib or _load(), name)(args, _stream(stream))
+    st = _fn(name)(args, _stream(stream))
     if st != FPDE_OK:
         raise FpdeError(st, name)
 
 
 def _workspace(name, args, dev, stream):
     """Allocates what the call needs and enters it in ``args``."""
-    n = getattr(_lib or _load(), name + "_workspace")(args)
+    n = _fn(name + "_workspace")(args)
     if n < 0:
         raise FpdeError(n, name)
     if n:
@@ -146,18 +155,25 @@ def _workspace(name, args, dev, stream):
 # Checks.  Sizes, strides and overlaps are checked by the C side too; here is
 # what only the tensors know: devices, types, and shapes that have to agree.
 
+# (Host time is what a call on a few rows costs, so the usual case is decided with
+# few attribute reads.)
+
+_Tensor, _F32 = torch.Tensor, torch.float32
+_device_now = torch.cuda.current_device
+
+
 def _data(what, t, dev=None, dtype=None):
     """A data tensor's type code; on the current device, or on ``dev``."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+    if not isinstance(t, _Tensor) or not t.is_cuda:
         raise ValueError(f"{what}: need a CUDA tensor")
-    code = _CODES.get(t.dtype)
-    if code is None or (dtype is not None and t.dtype is not dtype):
-        raise ValueError(f"{what}: dtype {t.dtype}, need " +
+    dt = t.dtype
+    code = _CODES.get(dt)
+    if code is None or (dtype is not None and dt is not dtype):
+        raise ValueError(f"{what}: dtype {dt}, need " +
                          (str(dtype) if dtype is not None else "float32, bfloat16 or float16"))
     if dev is None:
-        if t.device.index != torch.cuda.current_device():
-            raise ValueError(f"{what}: tensor on {t.device}, current device is "
-                             f"cuda:{torch.cuda.current_device()}")
+        if t.get_device() != _device_now():
+            raise ValueError(f"{what}: tensor on {t.device}, current device is cuda:{_device_now()}")
     elif t.device != dev:
         raise ValueError(f"{what}: tensors on different devices ({dev}, {t.device})")
     return code
@@ -181,11 +197,12 @@ def _param(what, t, shape, dtype, dev):
 def _rows(what, t):
     """(rows, width, row stride) of a tensor whose leading axes fold into one."""
     n = t.dim()
+    if n and t.is_contiguous():
+        width = t.shape[-1]
+        return (t.numel() // width if width else 0), width, width
     if n == 0 or (t.shape[-1] > 1 and t.stride(-1) != 1):
         raise ValueError(f"{what}: the last axis has to be dense")
     width = t.shape[-1]
-    if t.is_contiguous():
-        return (t.numel() // width if width else 0), width, width
     rows, stride = 1, width
     for a in range(n - 2, -1, -1):
         if t.shape[a] == 1:
@@ -209,6 +226,16 @@ def _levels(what, t):
 
 def _empty(stream, shape, dtype, dev):
     t = torch.empty(shape, dtype=dtype, device=dev)
+    if stream is not None:
+        _used_on(stream, t)
+    return t
+
+
+def _empty_like(stream, x):
+    """A dense tensor like x."""
+    if not x.is_contiguous():
+        return _empty(stream, x.shape, x.dtype, x.device)
+    t = torch.empty_like(x)
     if stream is not None:
         _used_on(stream, t)
     return t
@@ -238,7 +265,7 @@ def fpde_rms_norm(x, weight=None, *, residual=None, eps: float = 1e-6, quant: Op
     if sum_out is not None:
         sp = _dense("fpde_rms_norm sum_out", sum_out, x.shape, dt, dev)
     elif residual is not None:
-        sum_out = _empty(stream, x.shape, dt, dev)
+        sum_out = _empty_like(stream, x)
         sp = sum_out.data_ptr()
     wp, wcode = None, code
     if weight is not None:
@@ -246,7 +273,7 @@ def fpde_rms_norm(x, weight=None, *, residual=None, eps: float = 1e-6, quant: Op
     scales = None
     odt = dt if quant is None else torch.float8_e4m3fn
     if out is None:
-        out = _empty(stream, x.shape, odt, dev)
+        out = _empty_like(stream, x) if quant is None else _empty(stream, x.shape, odt, dev)
     else:
         _dense("fpde_rms_norm out", out, x.shape, odt, dev)
     if quant is not None:
@@ -284,7 +311,7 @@ def fpde_rms_norm_bwd(dy, s, weight=None, *, dsum=None, eps: float = 1e-6, want_
         if want_dweight:
             dweight = _empty(stream, (width,), weight.dtype, dev)
     if ds is None:
-        ds = _empty(stream, dy.shape, dt, dev)
+        ds = _empty_like(stream, dy)
     else:
         _dense("fpde_rms_norm_bwd ds", ds, dy.shape, dt, dev)
     a = NormBwdArgs(code, wcode, rows, width, dys, ss, dss, eps, dy.data_ptr(), s.data_ptr(), dp, wp,
@@ -354,13 +381,23 @@ def fpde_causal_conv(x, weight, bias=None, *, silu: bool = True, state=None, len
 def fpde_causal_conv_step(x, state, weight, bias=None, *, silu: bool = True, out=None, stream=None):
     """One level of ``fpde_causal_conv``: x [B, D]; ``state`` [B, taps - 1, D] is read
     and updated in place.  Returns y [B, D]."""
-    if not isinstance(x, torch.Tensor) or x.dim() != 2:
-        raise ValueError("fpde_causal_conv_step x: need [batch, channels]")
-    if state is None:
-        raise ValueError("fpde_causal_conv_step: needs a state")
-    y = fpde_causal_conv(x.unsqueeze(1), weight, bias, silu=silu, state=state, state_out=state,
-                         out=None if out is None else out.unsqueeze(1), stream=stream)
-    return y.squeeze(1)
+    what = "fpde_causal_conv_step"
+    code = _data(f"{what} x", x)
+    if x.dim() != 2 or not isinstance(weight, _Tensor) or weight.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
+        raise ValueError(f"{what}: need x [batch, channels] with dense channels and weight [channels, taps]")
+    dev, dt = x.device, x.dtype
+    B, D = x.shape
+    W = weight.shape[1]
+    if out is None:
+        out = _empty_like(stream, x)
+    else:
+        _dense(f"{what} out", out, x.shape, dt, dev)
+    wp = _param(f"{what} weight", weight, (D, W), dt, dev)
+    bp = None if bias is None else _dense(f"{what} bias", bias, (D,), weight.dtype, dev)
+    sp = _dense(f"{what} state", state, (B, W - 1, D), dt, dev)
+    _call("fpde_causal_conv", ConvArgs(code, _CODES[weight.dtype], W, bool(silu), B, 1, D, x.stride(0), D,
+                                       x.data_ptr(), wp, bp, sp, None, out.data_ptr(), sp), stream)
+    return out
 
 
 def fpde_causal_conv_bwd(dy, x, weight, bias=None, *, silu: bool = True, state=None, lengths=None, stream=None):
@@ -471,12 +508,42 @@ def fpde_selective_step(state, u, delta, A, B, C, *, D=None, z=None, delta_bias=
     """One level of ``fpde_selective_scan``: u, delta, z [b, channels], B, C [b, groups,
     states] or [b, states]; ``state`` [b, channels, states] is read and updated in
     place.  Returns y [b, channels]."""
-    if state is None or not isinstance(u, torch.Tensor) or u.dim() != 2:
-        raise ValueError("fpde_selective_step: needs a state and u [batch, channels]")
-    one = [None if t is None else t.unsqueeze(1) for t in (u, delta, B, C, z, out)]
-    y = fpde_selective_scan(one[0], one[1], A, one[2], one[3], D=D, z=one[4], delta_bias=delta_bias,
-                            softplus=softplus, state=state, state_out=state, out=one[5], stream=stream)
-    return y.squeeze(1)
+    what = "fpde_selective_step"
+    code = _data(f"{what} u", u)
+    if u.dim() != 2 or not isinstance(A, _Tensor) or A.dim() != 2:
+        raise ValueError(f"{what}: need u [batch, channels] and A [channels, states]")
+    dev, dt, f32 = u.device, u.dtype, _F32
+    Bn, Dn = u.shape
+    n = A.shape[1]
+    groups = B.shape[1] if isinstance(B, _Tensor) and B.dim() == 3 else 1
+    strides = []
+    for name, t in (("u", u), ("delta", delta), ("z", z)):
+        if t is None and name == "z":
+            strides += (0, 0)
+            continue
+        _data(f"{what} {name}", t, dev, dt)
+        if t.shape != u.shape or (Dn > 1 and t.stride(1) != 1):
+            raise ValueError(f"{what} {name}: need [batch, channels] like u, with dense channels")
+        strides += (t.stride(0), Dn)
+    for name, t in (("B", B), ("C", C)):
+        _data(f"{what} {name}", t, dev, dt)
+        if t.shape != (Bn, groups, n) and (groups > 1 or t.shape != (Bn, n)):
+            raise ValueError(f"{what} {name}: need [batch, groups, states] (or without groups)")
+        if (n > 1 and t.stride(-1) != 1) or (groups > 1 and t.stride(1) != n):
+            raise ValueError(f"{what} {name}: groups and states have to be dense")
+        strides += (t.stride(0), groups * n)
+    if out is None:
+        out = _empty_like(stream, u)
+    else:
+        _dense(f"{what} out", out, u.shape, dt, dev)
+    sp = _dense(f"{what} state", state, (Bn, Dn, n), f32, dev)
+    _call("fpde_selective_scan", ScanArgs(
+        code, n, groups, bool(softplus), Bn, 1, Dn, *strides, u.data_ptr(), delta.data_ptr(),
+        _dense(f"{what} A", A, (Dn, n), f32, dev), B.data_ptr(), C.data_ptr(),
+        None if D is None else _dense(f"{what} D", D, (Dn,), f32, dev), None if z is None else z.data_ptr(),
+        None if delta_bias is None else _dense(f"{what} delta_bias", delta_bias, (Dn,), f32, dev), sp, None,
+        out.data_ptr(), sp, None, 0), stream)
+    return out
 
 
 ScanGrads = namedtuple("ScanGrads", "du ddelta dA dB dC dD dz ddelta_bias")
