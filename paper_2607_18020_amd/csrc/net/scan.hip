@@ -5,12 +5,15 @@
 //   y_t = sum_n C_t h_t + D u_t,  out_t = y_t silu(z_t)
 //
 // A lane owns one channel and keeps its NS states in registers; neighbouring lanes
-// own neighbouring channels, so every access to u, delta, z and out is dense, and B
-// and C, the same for all channels of a group, are staged through LDS in float32
-// and read by broadcast.  Per level, channel and state: one product and one exp2
-// for a, then one product and two multiply-adds; the exponential counts as four of
-// those, so 16 states cost about 130 VALU slots and the operator is bound by the
-// VALU, not by its 4 reads and writes an element.
+// own neighbouring channels, so every access to u, delta, z and out is dense.  A
+// workgroup is one wavefront: nothing waits for another.  B and C, the same for all
+// channels of a group, go through 1 KB of LDS, a block of levels at a time: every lane
+// fetches four numbers of the next block while this one is worked on, writes them as
+// float32, and all lanes read them back by broadcast.  Per level, channel and state:
+// one product and one exp2 for a, then one product and two multiply-adds; an exp2 takes
+// the time of two, so 16 states cost about 100 VALU slots and the level itself (softplus,
+// gate, conversions) about 50, and the operator is bound by the VALU, not by its 4
+// reads and writes an element.
 //
 // Few sequences and channels leave the card empty, since time is serial: the window
 // is then split in chunks.  A first pass finds what each chunk adds to the state
@@ -23,21 +26,22 @@
 //   g_t = C_t dy_t + a_{t+1} g_{t+1};  dC_t = sum_c h_t dy_t;  dB_t = sum_c g_t dt_t u_t
 //   du_t = D dy_t + dt_t sum_n g_t B_t
 //   ddt_t = sum_n g_t (A a_t h_{t-1} + B_t u_t);  dA = sum_t dt_t g_t a_t h_{t-1}
-// One pass forward leaves the state at the start of every block of KB levels; the
-// main pass walks the blocks backward, runs each block forward again from its state
-// with all a_t h_{t-1} of the block in registers, and then backward.  The window is
-// split in chunks as above, with the same scan over chunks for g.  The sums over
-// channels (dB, dC) halve the values and the lanes together (reduce_lanes): one
-// swap or DPP and one addition for each value that goes; the wavefronts' sums meet
-// in LDS and the workgroups' in partial rows that a last launch adds in order.
+// One pass forward leaves the state at the start of every block of 8 levels (from zero at
+// the chunk's start where there are chunks, with the sum of dt to bring in the state
+// that the chunk starts from later), and, as sum_t (prod_{s<=t} a_s) C_t dy_t is what a
+// chunk hands to the adjoint before it, that too.  The main pass walks the blocks backward,
+// runs each block forward again from its state with all a_t h_{t-1} of the block in
+// registers, and then backward.  That takes 15 registers a state, so a lane has 8 states
+// at most and 2 or 4 lanes own a channel with more: one lane with 16 took 400 registers,
+// a single wavefront a SIMD.  The sums over channels (dB, dC) halve the values and the
+// lanes together (reduce_lanes): one swap or DPP and one addition for each value that
+// goes; the wavefronts' sums are partial rows that a last launch adds in order.
 #include "net_common.hpp"
 
 using namespace fpde_net;
 
 namespace {
 
-constexpr int kTile = 16;        // levels of B and C staged together
-constexpr int kSub = 8;          // levels whose loads are in flight together
 constexpr float kLn2 = 0.69314718055994530942f;
 
 struct Seq {  // a [batch][length][...] array
@@ -51,13 +55,27 @@ struct ScanP {
     const int32_t* lengths;
     void *y, *ddelta, *dz;                // y: du in the backward
     float* state_out;
-    float *hend, *gend, *sdt;             // [batch][chunks][states][channels], [batch][chunks][channels]
-    float* ck;                            // [batch][blocks][states][channels]
+    float *hend, *gend, *sdt;             // [batch][chunks][NS][channels], [batch][chunks][channels]
+    float *ck, *cs;                       // [batch][blocks][NS][channels], [batch][blocks][channels]
     float *pbc, *pA, *pD, *pbias;         // partial sums
-    int64_t batch;
-    int length, channels, states, groups, softplus;
-    int chunk, chunks, per, nblk, slots;  // per: channels a group; nblk: workgroups a group
+    int64_t batch, jobs;                  // jobs: sequences times chunks
+    int length, channels, states, groups, softplus, gate;  // (without a gate z is u, and not used)
+    int chunk, chunks, per, nblk;         // per: channels a group; nblk: wavefronts a group
+    int rows;                             // jobs that run at a time: a wavefront takes every rows-th
 };
+
+// The kernel's arguments, read again: held in scalar registers from a kernel's start to its end, the
+// pointers and strides of a dozen arrays would be moved to vector registers and back all the time.
+__device__ __forceinline__ ScanP args_again() {
+#ifdef __HIP_DEVICE_COMPILE__
+    typedef const __attribute__((address_space(4))) ScanP* args_t;
+    args_t p = (args_t)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *p;
+#else
+    return ScanP{};
+#endif
+}
 
 __device__ __forceinline__ int lane_levels(const int32_t* lengths, int64_t b, int length) {
     if (!lengths) return length;
@@ -73,7 +91,7 @@ __device__ __forceinline__ int levels(const int32_t* lengths, int64_t b, int len
 // log2(e) is carried to twice the precision, so that small results keep their digits;
 // log1p(e) = 2 artanh(e / (2 + e)), whose series in s^2 <= 1/9 is cut below 2^-26.
 __device__ __forceinline__ float softplus(float x) {
-    const float ax = -fabsf(x), hi = ax * kLog2e;
+    const float ax = fmaxf(-fabsf(x), -200.f), hi = ax * kLog2e;  // (e is 0 long before)
     const float lo = fmaf(ax, kLog2e, -hi) + ax * 1.92596299e-8f;  // log2(e) - float(log2(e))
     float e = __builtin_amdgcn_exp2f(hi);
     e = fmaf(e, lo * kLn2, e);
@@ -86,47 +104,59 @@ __device__ __forceinline__ float softplus(float x) {
     r = fmaf(r, q, 1.f / 5);
     r = fmaf(r, q, 1.f / 3);
     r = fmaf(r, q, 1.f);
-    const float v = fmaf(2.f * s, r, fmaxf(x, 0.f));
-    return x != x ? x : (ax < -3.0e38f ? fmaxf(x, 0.f) : v);  // (infinite x: no 0 * inf above)
+    return fmaf(2.f * s, r, x < 0.f ? 0.f : x);  // (NaN stays)
+}
+
+// (a select, not a branch: levels are one stretch of code.  The result is opaque, so that a level's
+// exponentials are not formed before it, all levels of a block together, for want of registers.)
+__device__ __forceinline__ float step_of(const ScanP& P, float raw) {
+    const float v = softplus(raw);
+    float dt = P.softplus ? v : raw;
+    asm volatile("" : "+v"(dt));
+    return dt;
 }
 
 // ---------------------------------------------------------------------------
-// A workgroup's place: its channels within one group, and one lane's channel.
-
+// A wavefront's place: its row of jobs, and its channels within one group.
 struct Place {
-    int g, c;
+    int row, blk, g, c, part;
     bool live;
 };
-template <int TPB>
-__device__ __forceinline__ Place place(const ScanP& P, int blk) {
+// LP lanes own a channel, 64 / LP apart, with a part of its states each.
+template <int LP = 1>
+__device__ __forceinline__ Place place(const ScanP& P) {
     Place q;
-    q.g = blk / P.nblk;
-    const int l = (blk - q.g * P.nblk) * TPB + (int)threadIdx.x;
+    const int w = P.nblk * P.groups;
+    q.row = (int)blockIdx.x / w;
+    q.blk = (int)blockIdx.x - q.row * w;
+    q.g = q.blk / P.nblk;
+    constexpr int CH = 64 / LP;
+    q.part = (int)threadIdx.x / CH;
+    const int l = (q.blk - q.g * P.nblk) * CH + (int)threadIdx.x % CH;
     q.live = l < P.per;
-    q.c = q.g * P.per + (q.live ? l : P.per - 1);  // (idle lanes repeat the last channel and store nothing)
+    // Lanes past the last channel repeat it: what they store is the same once more, and where lanes are
+    // added up they count as 0 (live).
+    q.c = q.g * P.per + (q.live ? l : P.per - 1);
     return q;
 }
 
-// B and C of levels t .. t + TL - 1 (those before t1; zeros after) into bc[TL][2 NS]
-template <class T, int NS, int TPB, int TL, bool WITH_C>
-__device__ __forceinline__ void stage_bc(const ScanP& P, int64_t b, int g, int t, int t1, float* bc) {
-    constexpr int E = TL * NS;
-#pragma unroll
-    for (int h = 0; h < (WITH_C ? 2 : 1); ++h) {
-        const Seq& s = h ? P.C : P.B;
-        const T* p = (const T*)s.p + b * s.bs + (int64_t)g * P.states;
-#pragma unroll
-        for (int e0 = 0; e0 < E; e0 += TPB) {
-            const int e = e0 + (int)threadIdx.x, j = e / NS, n = e % NS;
-            if (E % TPB == 0 || e < E) {
-                const bool in = n < P.states && t + j < t1;
-                bc[j * 2 * NS + h * NS + n] = in ? to_f32<T>(p[(int64_t)(t + j) * s.ts + n]) : 0.f;
-            }
-        }
-    }
+// The chunk that a job is: sequence b, levels t0 .. tn - 1, of which those before t1 exist.
+struct Job {
+    int64_t b;
+    int ch, t0, tn, t1;
+};
+__device__ __forceinline__ Job job_of(const ScanP& P, int64_t i) {
+    Job j;
+    j.b = P.chunks == 1 ? i : i / P.chunks;
+    j.ch = P.chunks == 1 ? 0 : (int)(i - j.b * P.chunks);
+    const int len = levels(P.lengths, j.b, P.length);
+    j.t0 = j.ch * P.chunk;
+    j.tn = j.t0 + P.chunk < P.length ? j.t0 + P.chunk : P.length;
+    j.t1 = j.tn < len ? j.tn : len;
+    return j;
 }
 
-// (the row's address is the workgroup's, so only the channel takes a lane's register)
+// (the row's address is the wavefront's, so only the channel takes a lane's register)
 template <class T>
 __device__ __forceinline__ T at(const Seq& s, int64_t b, int t, int c) {
     return ((const T*)s.p + b * s.bs + (int64_t)t * s.ts)[(unsigned)c];
@@ -136,119 +166,311 @@ __device__ __forceinline__ void put(void* p, int64_t row, int channels, int c, f
     ((T*)p + row * channels)[(unsigned)c] = from_f32<T>(v);
 }
 
+// B and C of a block of K levels in LDS: row j holds B's NS numbers, then C's (zeros past the states
+// that exist).  Four neighbouring numbers are a lane's; a lane has Q such quads.
+template <class T, int NS, int K>
+struct Tile {
+    static constexpr int ROW = 2 * NS, QUADS = K * ROW / 4, Q = (QUADS + 63) / 64;
+    Raw<T, 4> q[Q];
+    // starts the loads of levels t .. t + K - 1 (those from t1 on are the last one again)
+    __device__ __forceinline__ void load(const ScanP& P, int64_t b, int g, int t, int t1) {
+#pragma unroll
+        for (int i = 0; i < Q; ++i) {
+            const int e = i * 64 + (int)threadIdx.x, j = e / (ROW / 4), r = e % (ROW / 4) * 4;
+            const bool is_c = r >= NS;
+            int n = is_c ? r - NS : r;
+            const int l = t + j < t1 ? t + j : t1 - 1;
+            const T* p = (const T*)(is_c ? P.C.p : P.B.p) + b * (is_c ? P.C.bs : P.B.bs) +
+                         (int64_t)l * (is_c ? P.C.ts : P.B.ts) + (int64_t)g * P.states;
+            if (P.states % 4 == 0) {
+                q[i] = load_raw<T, 4>(p + (n < P.states ? n : 0));
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) q[i][k] = p[n + k < P.states ? n + k : 0];
+            }
+        }
+    }
+    __device__ __forceinline__ void store(const ScanP& P, float* lds) const {
+#pragma unroll
+        for (int i = 0; i < Q; ++i) {
+            const int e = i * 64 + (int)threadIdx.x, r = e % (ROW / 4) * 4, n = r >= NS ? r - NS : r;
+            float4 v;
+            v.x = n < P.states ? to_f32<T>(q[i][0]) : 0.f;
+            v.y = n + 1 < P.states ? to_f32<T>(q[i][1]) : 0.f;
+            v.z = n + 2 < P.states ? to_f32<T>(q[i][2]) : 0.f;
+            v.w = n + 3 < P.states ? to_f32<T>(q[i][3]) : 0.f;
+            if (QUADS % 64 == 0 || e < QUADS) *(float4*)(lds + e * 4) = v;
+        }
+        // (one wavefront: its LDS accesses are carried out in order)
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+};
+
+// The number of states, such that what is compared with it is compared where it is used: hoisted out of
+// the loops the comparisons of every n would fill the scalar registers.
+__device__ __forceinline__ int states_here(const ScanP& P) {
+    int n = P.states;
+    asm volatile("" : "+s"(n));
+    return n;
+}
 // A * log2(e) of one channel (0 past the states that exist)
 template <int NS>
 __device__ __forceinline__ void load_a2(const ScanP& P, int c, float (&a2)[NS]) {
+    const int k = states_here(P);
 #pragma unroll
-    for (int n = 0; n < NS; ++n) a2[n] = n < P.states ? P.A[(int64_t)c * P.states + n] * kLog2e : 0.f;
+    for (int n = 0; n < NS; ++n) a2[n] = n < k ? P.A[(int64_t)c * k + n] * kLog2e : 0.f;
+}
+// the carried state of one channel, or zeros
+template <int NS>
+__device__ __forceinline__ void load_carried(float (&h)[NS], const ScanP& P, int64_t b, int c) {
+    const int k = states_here(P);
+    const float* s = P.state ? P.state + (b * P.channels + c) * k : nullptr;
+#pragma unroll
+    for (int n = 0; n < NS; ++n) h[n] = s && n < k ? s[n] : 0.f;
+}
+// a row of states, [NS][channels] from p on (those past the states that exist are 0 throughout)
+template <int NS>
+__device__ __forceinline__ void load_states(float (&h)[NS], const float* p, const ScanP& P, int c) {
+#pragma unroll
+    for (int n = 0; n < NS; ++n, p += P.channels) h[n] = p[(unsigned)c];
+}
+template <int NS>
+__device__ __forceinline__ void store_states(const float (&h)[NS], float* p, const ScanP& P, int c) {
+#pragma unroll
+    for (int n = 0; n < NS; ++n, p += P.channels) p[(unsigned)c] = h[n];
 }
 
 // ---------------------------------------------------------------------------
-// Forward.  OUT: the outputs.  ENDS: a chunk's own contribution to the state, from zero,
-// and its sum of dt.  CHECKS: the state at the start of every block of KB levels.
-enum { OUT, ENDS, CHECKS };
+// Forward.  OUT: the outputs.  ENDS: a chunk's own contribution to the state, from zero, and its
+// sum of dt.
 
-template <class T, int NS, int TPB, int MODE, int KB>
-__global__ __launch_bounds__(TPB) void scan_fwd_kernel(ScanP P) {
-    __shared__ __attribute__((aligned(16))) float bc[kTile * 2 * NS];
-    const int64_t job = (int64_t)(blockIdx.x / (P.nblk * P.groups));
-    const Place q = place<TPB>(P, (int)(blockIdx.x % (P.nblk * P.groups)));
-    const int64_t b = job / P.chunks;
-    const int ch = (int)(job - b * P.chunks), c = q.c;
-    const int len = levels(P.lengths, b, P.length);
-    const int t0 = ch * P.chunk, tn = t0 + P.chunk < P.length ? t0 + P.chunk : P.length;
-    const int t1 = tn < len ? tn : len;
-    float a2[NS], h[NS];
-    load_a2<NS>(P, c, a2);
-    const float bias = P.bias ? P.bias[c] : 0.f, dd = MODE == OUT && P.D ? P.D[c] : 0.f;
-    if (MODE != ENDS && P.chunks > 1) {
-        const float* s = P.hend + job * P.states * P.channels + c;
-#pragma unroll
-        for (int n = 0; n < NS; ++n) h[n] = n < P.states ? s[(int64_t)n * P.channels] : 0.f;
-    } else {
-        const float* s = MODE != ENDS && P.state ? P.state + (b * P.channels + c) * P.states : nullptr;
-#pragma unroll
-        for (int n = 0; n < NS; ++n) h[n] = s && n < P.states ? s[n] : 0.f;
+// A row that moves with time.  Its pointer is the wavefront's and advances by one addition a level, so
+// that the levels in flight do not each hold an address.
+template <class T>
+struct Cursor {
+    const T* p;
+    int64_t ts;
+    __device__ __forceinline__ void set(const Seq& s, int64_t b, int t) {
+        p = (const T*)s.p + b * s.bs + (int64_t)t * s.ts;
+        ts = s.ts;
     }
-    float sum = 0.f;
-    const int64_t row = b * P.length;
-    for (int tt = t0; tt < t1; tt += kTile) {
-        __syncthreads();
-        stage_bc<T, NS, TPB, kTile, MODE == OUT>(P, b, q.g, tt, t1, bc);
-        __syncthreads();
+    // this level's value; `more`: there is another level after it
+    __device__ __forceinline__ T next(int c, bool more) {
+        const T v = p[(unsigned)c];
+        p += more ? ts : 0;
+        return v;
+    }
+};
+
+// the inputs of K levels from t on (past the last level it again)
+template <class T, int K>
+struct Block {
+    T u[K], d[K], z[K], g[K];
+};
+template <class T>
+struct Cursors {
+    Cursor<T> u, d, z, g;
+    bool gate, grad;
+    __device__ __forceinline__ void set(const ScanP& P, int64_t b, int t, bool with_z, bool with_dy) {
+        gate = with_z, grad = with_dy;
+        u.set(P.u, b, t), d.set(P.delta, b, t);
+        if (gate) z.set(P.z, b, t);
+        if (grad) g.set(P.dy, b, t);
+    }
+    template <int K>
+    __device__ __forceinline__ void load(Block<T, K>& q, int t, int t1, int c) {
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            const bool more = t + j + 1 < t1;
+            q.u[j] = u.next(c, more);
+            q.d[j] = d.next(c, more);
+            if (gate) q.z[j] = z.next(c, more);
+            if (grad) q.g[j] = g.next(c, more);
+        }
+    }
+};
+
+// Levels are not mixed: the registers hold one level's B, C and products, not a block's.
+__device__ __forceinline__ void level_fence() {
+    __builtin_amdgcn_sched_barrier(0);
+}
+// Level j of a tile.  The offset is opaque, so that its reads stay with the level and are not brought
+// forward to the block's start, which would take a register for every number of the tile.
+template <int NS>
+struct Row {
+    const float4* p;
+    __device__ __forceinline__ float operator[](int n) const {
+        const float4 v = p[n >> 2];
+        return (n & 3) == 0 ? v.x : (n & 3) == 1 ? v.y : (n & 3) == 2 ? v.z : v.w;
+    }
+};
+template <int NS>
+__device__ __forceinline__ Row<NS> row_of(const float* bc, int j, int n0 = 0) {
+    int o = j * (NS / 2) + n0 / 4;
+    asm volatile("" : "+v"(o));
+    return Row<NS>{(const float4*)bc + o};
+}
+// f(j) for the first n of a block's K levels
+template <int K, class F>
+__device__ __forceinline__ void in_block(int n, F f) {
+    if (n >= K) {
+        level_fence();
+#pragma unroll
+        for (int j = 0; j < K; ++j) f(j);
+    } else {
+        level_fence();
+#pragma unroll
+        for (int j = 0; j < K - 1; ++j)
+            if (j < n) f(j);
+    }
+}
+// the same with a branch a level, in order and back
+template <int K, class F>
+__device__ __forceinline__ void guarded(int n, F f) {
+#pragma unroll
+    for (int j = 0; j < K; ++j)
+        if (j < n) f(j);
+}
+template <int K, class F>
+__device__ __forceinline__ void back_guarded(int n, F f) {
+#pragma unroll
+    for (int j = K - 1; j >= 0; --j)
+        if (j < n) f(j);
+}
+
+template <class T, int NS, bool OUT>
+__global__ __launch_bounds__(64) void scan_fwd_kernel(ScanP P) {
+    constexpr int K = 8;
+    __shared__ __attribute__((aligned(16))) float bc[K * 2 * NS];
+    const Place q = place(P);
+    const int c = q.c;
+    float a2[NS];
+    load_a2<NS>(P, c, a2);
+    const float bias = P.bias ? P.bias[c] : 0.f, dd = OUT && P.D ? P.D[c] : 0.f;
+    for (int64_t i = q.row; i < P.jobs; i += P.rows) {
+        const Job J = job_of(P, i);
+        Block<T, K> now, next;
+        Cursors<T> in;
+        in.set(P, J.b, J.t0, OUT, false);
+        Tile<T, NS, K> tile;
+        if (J.t0 < J.t1) {
+            tile.load(P, J.b, q.g, J.t0, J.t1);
+            in.load(now, J.t0, J.t1, c);
+        }
+        T* out = (T*)P.y + (J.b * P.length + J.t0) * P.channels;
+        float h[NS];
+        if (OUT && P.chunks > 1) {
+            load_states<NS>(h, P.hend + i * NS * P.channels, P, c);
+        } else if (OUT) {
+            load_carried<NS>(h, P, J.b, c);
+        } else {
+#pragma unroll
+            for (int n = 0; n < NS; ++n) h[n] = 0.f;
+        }
+        float sum = 0.f;
+        const int64_t row = J.b * P.length;
 #pragma unroll 1
-        for (int t = tt; t < tt + kTile && t < t1; t += kSub) {
-            T ru[kSub], rd[kSub], rz[kSub];
-#pragma unroll
-            for (int j = 0; j < kSub; ++j) {
-                const int s = t + j < t1 ? t + j : t1 - 1;
-                ru[j] = at<T>(P.u, b, s, c);
-                rd[j] = at<T>(P.delta, b, s, c);
-                if (MODE == OUT && P.z.p) rz[j] = at<T>(P.z, b, s, c);
+        for (int t = J.t0; t < J.t1; t += K) {
+            const ScanP Q = args_again();
+            tile.store(Q, bc);
+            if (t + K < J.t1) {
+                tile.load(Q, J.b, q.g, t + K, J.t1);
+                in.load(next, t + K, J.t1, c);
             }
-#pragma unroll
-            for (int j = 0; j < kSub; ++j) {
-                if (t + j >= t1) break;
-                if (MODE == CHECKS && (t + j - t0) % KB == 0 && q.live) {
-                    const int64_t blocks = (P.length + KB - 1) / KB;
-                    float* s = P.ck + (b * blocks + (t + j) / KB) * P.states * P.channels;
-#pragma unroll
-                    for (int n = 0; n < NS; ++n)
-                        if (n < P.states) (s + (int64_t)n * P.channels)[(unsigned)c] = h[n];
-                }
-                const float* w = bc + (t - tt + j) * 2 * NS;
-                const float u = to_f32<T>(ru[j]), raw = to_f32<T>(rd[j]) + bias;
-                const float dt = P.softplus ? softplus(raw) : raw, du = dt * u;
+            // (whole blocks run without a branch between levels)
+            in_block<K>(J.t1 - t, [&](int j) {
+                const Row<NS> w = row_of<NS>(bc, j);
+                const float u = to_f32<T>(now.u[j]), raw = to_f32<T>(now.d[j]) + bias;
+                const float dt = step_of(P, raw), du = dt * u;
                 float acc = 0.f;
 #pragma unroll
                 for (int n = 0; n < NS; ++n) {
-                    const float a = __builtin_amdgcn_exp2f(dt * a2[n]);
-                    h[n] = fmaf(a, h[n], du * w[n]);
-                    if (MODE == OUT) acc = fmaf(h[n], w[NS + n], acc);
+                    h[n] = fmaf(__builtin_amdgcn_exp2f(dt * a2[n]), h[n], du * w[n]);
+                    if (OUT) acc = fmaf(h[n], w[NS + n], acc);
                 }
-                if (MODE == ENDS) sum += dt;
-                if (MODE == OUT) {
+                if (!OUT) sum += dt;
+                if (OUT) {
                     acc = fmaf(dd, u, acc);
-                    if (P.z.p) acc *= silu(to_f32<T>(rz[j]));
-                    if (q.live) put<T>(P.y, row + t + j, P.channels, c, acc);
+                    const float z = silu(to_f32<T>(now.z[j]));
+                    out[(unsigned)c] = from_f32<T>(P.gate ? acc * z : acc);
+                    out += P.channels;
                 }
+                level_fence();
+            });
+            now = next;
+        }
+        if (OUT) {
+            for (int t = J.t1 > J.t0 ? J.t1 : J.t0; t < J.tn; ++t) put<T>(P.y, row + t, P.channels, c, 0.f);
+            if (P.state_out && J.ch == P.chunks - 1) {
+                const int k = states_here(P);
+                float* s = P.state_out + (J.b * P.channels + c) * k;
+#pragma unroll
+                for (int n = 0; n < NS; ++n)
+                    if (q.live && n < k) s[n] = h[n];
             }
+        } else {
+            store_states<NS>(h, P.hend + i * NS * P.channels, P, c);
+            P.sdt[i * P.channels + c] = sum;
         }
-    }
-    if (!q.live) return;
-    if (MODE == OUT) {
-        for (int t = t1 > t0 ? t1 : t0; t < tn; ++t) put<T>(P.y, row + t, P.channels, c, 0.f);
-        if (P.state_out && ch == P.chunks - 1) {
-            float* s = P.state_out + (b * P.channels + c) * P.states;
-#pragma unroll
-            for (int n = 0; n < NS; ++n)
-                if (n < P.states) s[n] = h[n];
-        }
-    }
-    if (MODE == ENDS) {
-        float* s = P.hend + job * P.states * P.channels + c;
-#pragma unroll
-        for (int n = 0; n < NS; ++n)
-            if (n < P.states) s[(int64_t)n * P.channels] = h[n];
-        P.sdt[job * P.channels + c] = sum;
     }
 }
 
-// The state that every chunk starts from (e: what the chunks add, replaced by what they
-// start from), forward in time, or backward for the adjoint.  One lane a state.
-__global__ __launch_bounds__(256) void chunk_kernel(ScanP P, float* e, int backward) {
-    const int c = (int)(blockIdx.x * 256 + threadIdx.x), n = (int)blockIdx.y;
-    if (c >= P.channels) return;
+// The state that every chunk starts from, in place of what each adds (e): forward in time
+// (blockIdx.z 0), or backward for the adjoint (1, into e2).  A lane owns a state; a wavefront
+// takes 32 chunks, whose loads are all in flight together; up to 8 wavefronts meet in LDS.
+__global__ __launch_bounds__(512) void chunk_kernel(ScanP P, int ns, float* e, float* e2) {
+    constexpr int SEG = 32;
+    __shared__ float decay[8][64], add[8][64], carry[64];
+    const int W = (int)(blockDim.x >> 6);
+    const int lane = (int)(threadIdx.x & 63), wave = (int)(threadIdx.x >> 6), n = (int)blockIdx.y % P.states;
+    const bool back = blockIdx.z != 0;
+    const int cl = (int)blockIdx.x * 64 + lane, c = cl < P.channels ? cl : P.channels - 1;
     const float a2 = P.A[(int64_t)c * P.states + n] * kLog2e;
-    for (int64_t b = blockIdx.z; b < P.batch; b += gridDim.z) {
-        float h = !backward && P.state ? P.state[(b * P.channels + c) * P.states + n] : 0.f;
-#pragma unroll 4
-        for (int i = 0; i < P.chunks; ++i) {
-            const int64_t job = b * P.chunks + (backward ? P.chunks - 1 - i : i);
-            float* s = e + (job * P.states + n) * P.channels + c;
-            const float add = *s, sum = P.sdt[job * P.channels + c];
-            *s = h;
-            h = fmaf(sum == 0.f ? 1.f : __builtin_amdgcn_exp2f(sum * a2), h, add);
+    for (int64_t b = blockIdx.y / (unsigned)P.states; b < P.batch; b += gridDim.y / (unsigned)P.states) {
+        __syncthreads();
+        if (wave == 0) carry[lane] = !back && P.state ? P.state[(b * P.channels + c) * P.states + n] : 0.f;
+        for (int i0 = 0; i0 < P.chunks; i0 += W * SEG) {
+            float d[SEG], v[SEG];
+            const int first = i0 + wave * SEG;
+            const bool idle = first >= P.chunks;  // (a wavefront without chunks only keeps the barriers)
+            auto job = [&](int k) {
+                const int i = first + k < P.chunks ? first + k : P.chunks - 1;
+                return b * P.chunks + (back ? P.chunks - 1 - i : i);
+            };
+            float* s = back ? e2 : e;
+            if (!idle) {
+#pragma unroll
+                for (int k = 0; k < SEG; ++k) {
+                    d[k] = P.sdt[job(k) * P.channels + c];
+                    v[k] = s[(job(k) * ns + n) * P.channels + c];
+                }
+            }
+            float dp = 1.f, hp = 0.f;
+            if (!idle) {
+#pragma unroll
+                for (int k = 0; k < SEG; ++k) {
+                    const bool in = first + k < P.chunks;
+                    d[k] = in && d[k] != 0.f ? __builtin_amdgcn_exp2f(d[k] * a2) : 1.f;
+                    v[k] = in ? v[k] : 0.f;
+                    dp *= d[k];
+                    hp = fmaf(d[k], hp, v[k]);
+                }
+            }
+            decay[wave][lane] = dp, add[wave][lane] = hp;
+            __syncthreads();
+            float h = carry[lane];
+            for (int w = 0; w < wave; ++w) h = fmaf(decay[w][lane], h, add[w][lane]);
+            if (!idle) {
+#pragma unroll
+                for (int k = 0; k < SEG; ++k) {
+                    if (first + k < P.chunks && cl < P.channels) s[(job(k) * ns + n) * P.channels + c] = h;
+                    h = fmaf(d[k], h, v[k]);
+                }
+            }
+            __syncthreads();
+            if (wave == W - 1) carry[lane] = h;
+            __syncthreads();
         }
     }
 }
@@ -279,14 +501,14 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanP P) {
                 load_f32<T, 4>(C, (const T*)P.C.p + b * P.C.bs + (int64_t)g * P.states + n0, k);
             }
             const float u = to_f32<T>(at<T>(P.u, b, 0, cc)), raw = to_f32<T>(at<T>(P.delta, b, 0, cc)) + bias;
-            const float dt = P.softplus ? softplus(raw) : raw, du = dt * u;
+            const float dt = step_of(P, raw), du = dt * u;
 #pragma unroll
             for (int n = 0; n < 4; ++n) {
                 h[n] = fmaf(__builtin_amdgcn_exp2f(dt * (a[n] * kLog2e)), h[n], du * B[n]);
                 y = fmaf(h[n], C[n], y);
             }
             y = fmaf(dd, u, lanes_reduce<LPC, AddOp>(y));
-            if (P.z.p) y *= silu(to_f32<T>(at<T>(P.z, b, 0, cc)));
+            if (P.gate) y *= silu(to_f32<T>(at<T>(P.z, b, 0, cc)));
         }
         if (live && n0 == 0) ((T*)P.y)[b * P.channels + c] = from_f32<T>(y);
         if (live && k > 0 && P.state_out) store_f32<float, 4>(P.state_out + at_h, h, k);
@@ -296,60 +518,80 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanP P) {
 // ---------------------------------------------------------------------------
 // Backward.
 
-// What a chunk adds to the adjoint state that leaves it at its start: g through it
-// from zero at its end.
-template <class T, int NS, int TPB>
-__global__ __launch_bounds__(TPB) void scan_adj_kernel(ScanP P) {
-    __shared__ __attribute__((aligned(16))) float bc[kTile * 2 * NS];
-    const int64_t job = (int64_t)(blockIdx.x / (P.nblk * P.groups));
-    const Place q = place<TPB>(P, (int)(blockIdx.x % (P.nblk * P.groups)));
-    const int64_t b = job / P.chunks;
-    const int ch = (int)(job - b * P.chunks), c = q.c;
-    const int len = levels(P.lengths, b, P.length);
-    const int t0 = ch * P.chunk, tn = t0 + P.chunk < P.length ? t0 + P.chunk : P.length;
-    const int t1 = tn < len ? tn : len;
-    float a2[NS], g[NS];
+// Forward through the window: the state at the start of every block of KB levels.  SPLIT: from zero
+// at the chunk's start, with the sum of dt before the block; and what the chunk adds to the state after it and
+// to the adjoint state before it.
+template <class T, int NS, int KB, bool SPLIT>
+__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2))) void scan_pre_kernel(ScanP P) {
+    __shared__ __attribute__((aligned(16))) float bc[KB * 2 * NS];
+    constexpr bool AHEAD = !SPLIT || NS < 32;  // (4 x 32 numbers of state leave no room for a block ahead)
+    const Place q = place(P);
+    const int c = q.c;
+    const int64_t blocks = (P.length + KB - 1) / KB;
+    float a2[NS];
     load_a2<NS>(P, c, a2);
     const float bias = P.bias ? P.bias[c] : 0.f;
+    for (int64_t i = q.row; i < P.jobs; i += P.rows) {
+        const Job J = job_of(P, i);
+        Block<T, KB> now, next;
+        Cursors<T> in;
+        in.set(P, J.b, J.t0, SPLIT, SPLIT);
+        Tile<T, NS, KB> tile;
+        if (J.t0 < J.t1) {
+            tile.load(P, J.b, q.g, J.t0, J.t1);
+            in.load(now, J.t0, J.t1, c);
+        }
+        float h[NS], G[NS], prod[NS], sum = 0.f;
+        if (!SPLIT) load_carried<NS>(h, P, J.b, c);
 #pragma unroll
-    for (int n = 0; n < NS; ++n) g[n] = 0.f;
-    for (int tt = t0 + (t1 - t0 - 1) / kTile * kTile; t1 > t0 && tt >= t0; tt -= kTile) {
-        __syncthreads();
-        stage_bc<T, NS, TPB, kTile, true>(P, b, q.g, tt, t1, bc);
-        __syncthreads();
+        for (int n = 0; n < NS; ++n) h[n] = SPLIT ? 0.f : h[n], G[n] = 0.f, prod[n] = 1.f;
 #pragma unroll 1
-        for (int t = tt + kTile - kSub; t >= tt; t -= kSub) {
-            if (t >= t1) continue;
-            T ry[kSub], rd[kSub], rz[kSub];
-#pragma unroll
-            for (int j = 0; j < kSub; ++j) {
-                const int s = t + j < t1 ? t + j : t1 - 1;
-                ry[j] = at<T>(P.dy, b, s, c);
-                rd[j] = at<T>(P.delta, b, s, c);
-                if (P.z.p) rz[j] = at<T>(P.z, b, s, c);
+        for (int t = J.t0; t < J.t1; t += KB) {
+            const ScanP Q = args_again();
+            tile.store(Q, bc);
+            if (t + KB < J.t1) {
+                tile.load(Q, J.b, q.g, t + KB, J.t1);
+                if (AHEAD) in.load(next, t + KB, J.t1, c);
             }
+            const int64_t k = J.b * blocks + t / KB;
+            store_states<NS>(h, Q.ck + k * NS * P.channels, P, c);
+            if (SPLIT) (Q.cs + k * P.channels)[(unsigned)c] = sum;
+            in_block<KB>(J.t1 - t, [&](int j) {
+                const Row<NS> w = row_of<NS>(bc, j);
+                const float u = to_f32<T>(now.u[j]), raw = to_f32<T>(now.d[j]) + bias;
+                const float dt = step_of(P, raw), du = dt * u;
+                float dy = 0.f;
+                if (SPLIT) {
+                    dy = to_f32<T>(now.g[j]);
+                    const float z = silu(to_f32<T>(now.z[j]));
+                    dy = P.gate ? dy * z : dy;
+                    sum += dt;
+                }
 #pragma unroll
-            for (int j = kSub - 1; j >= 0; --j) {
-                if (t + j >= t1) continue;
-                const float* w = bc + (t - tt + j) * 2 * NS + NS;
-                const float raw = to_f32<T>(rd[j]) + bias, dt = P.softplus ? softplus(raw) : raw;
-                float dy = to_f32<T>(ry[j]);
-                if (P.z.p) dy *= silu(to_f32<T>(rz[j]));
-#pragma unroll
-                for (int n = 0; n < NS; ++n)
-                    g[n] = __builtin_amdgcn_exp2f(dt * a2[n]) * fmaf(w[n], dy, g[n]);
-            }
+                for (int n = 0; n < NS; ++n) {
+                    const float a = __builtin_amdgcn_exp2f(dt * a2[n]);
+                    h[n] = fmaf(a, h[n], du * w[n]);
+                    if (SPLIT) {
+                        prod[n] *= a;
+                        G[n] = fmaf(prod[n], dy * w[NS + n], G[n]);
+                    }
+                }
+                level_fence();
+            });
+            if (AHEAD)
+                now = next;
+            else if (t + KB < J.t1)
+                in.load(now, t + KB, J.t1, c);
+        }
+        if (SPLIT) {
+            store_states<NS>(h, P.hend + i * NS * P.channels, P, c);
+            store_states<NS>(G, P.gend + i * NS * P.channels, P, c);
+            P.sdt[i * P.channels + c] = sum;
         }
     }
-    if (!q.live) return;
-    float* s = P.gend + job * P.states * P.channels + c;
-#pragma unroll
-    for (int n = 0; n < NS; ++n)
-        if (n < P.states) s[(int64_t)n * P.channels] = g[n];
 }
 
-// Sums of NV values over the 64 lanes, NV a power of two up to 64: lane l ends with the
-// sum of value l / (64 / NV).  A step takes the values in pairs and keeps one of each on
+// Sums of values over lanes.  A step takes the values in pairs and keeps one of each on
 // the lanes with a bit clear and the other on those with it set, with the partner's
 // share added, so values and lanes halve together.
 __device__ __forceinline__ float pair_sum32(float a, float b) {
@@ -372,163 +614,184 @@ __device__ __forceinline__ float pair_sum_mirror(float a, float b, bool upper) {
     return upper ? y : x;
 }
 
-template <int NV>
+// One step over lane bit B: pairs become single values, or a single one is added up.
+template <int B, int N>
+__device__ __forceinline__ void reduce_step(float* v, int lane) {
+    constexpr int H = N > 1 ? N / 2 : 1;
+#pragma unroll
+    for (int i = 0; i < H; ++i) {
+        const float a = v[i], b = v[N > 1 ? i + H : i];
+        if constexpr (B == 5) v[i] = pair_sum32(a, b);
+        if constexpr (B == 4) v[i] = pair_sum16(a, b);
+        if constexpr (B == 3) v[i] = N > 1 ? pair_sum<0x128>(a, b, lane & 8) : a + dpp<0x128>(a);
+        if constexpr (B == 2) v[i] = N > 1 ? pair_sum_mirror<0x141>(a, b, lane & 4) : a + dpp<0x141>(a);
+        if constexpr (B == 1) v[i] = N > 1 ? pair_sum<0x4E>(a, b, lane & 2) : a + dpp<0x4E>(a);
+        if constexpr (B == 0) v[i] = N > 1 ? pair_sum<0xB1>(a, b, lane & 1) : a + dpp<0xB1>(a);
+    }
+}
+template <int B, int N>
+__device__ __forceinline__ void reduce_bits(float* v, int lane) {
+    reduce_step<B, N>(v, lane);
+    if constexpr (B > 0) reduce_bits<B - 1, (N > 1 ? N / 2 : 1)>(v, lane);
+}
+// Sums of NV values over groups of 64 / LP lanes: lane l of a group ends with that of value
+// l / (64 / LP / NV).
+template <int NV, int LP>
 __device__ __forceinline__ float reduce_lanes(float (&v)[NV]) {
-    const int lane = (int)(threadIdx.x & 63);
-    constexpr int N1 = NV > 1 ? NV / 2 : 1;
-#pragma unroll
-    for (int i = 0; i < N1; ++i) v[i] = pair_sum32(v[i], v[NV > 1 ? i + N1 : i]);
-    constexpr int N2 = N1 > 1 ? N1 / 2 : 1;
-#pragma unroll
-    for (int i = 0; i < N2; ++i) v[i] = pair_sum16(v[i], v[N1 > 1 ? i + N2 : i]);
-    constexpr int N3 = N2 > 1 ? N2 / 2 : 1;
-#pragma unroll
-    for (int i = 0; i < N3; ++i)
-        v[i] = N2 > 1 ? pair_sum<0x128>(v[i], v[N2 > 1 ? i + N3 : i], lane & 8) : v[i] + dpp<0x128>(v[i]);
-    constexpr int N4 = N3 > 1 ? N3 / 2 : 1;
-#pragma unroll
-    for (int i = 0; i < N4; ++i)
-        v[i] = N3 > 1 ? pair_sum_mirror<0x141>(v[i], v[N3 > 1 ? i + N4 : i], lane & 4)
-                      : v[i] + dpp<0x141>(v[i]);
-    constexpr int N5 = N4 > 1 ? N4 / 2 : 1;
-#pragma unroll
-    for (int i = 0; i < N5; ++i)
-        v[i] = N4 > 1 ? pair_sum<0x4E>(v[i], v[N4 > 1 ? i + N5 : i], lane & 2) : v[i] + dpp<0x4E>(v[i]);
-    return N5 > 1 ? pair_sum<0xB1>(v[0], v[N5 > 1 ? 1 : 0], lane & 1) : v[0] + dpp<0xB1>(v[0]);
+    reduce_bits<(LP == 1 ? 5 : LP == 2 ? 4 : 3), NV>(v, (int)threadIdx.x);
+    return v[0];
+}
+// The sum over a channel's LP lanes, in each of them.
+template <int LP>
+__device__ __forceinline__ float parts_sum(float v) {
+    if constexpr (LP >= 2) v = pair_sum32(v, v);
+    if constexpr (LP >= 4) v = pair_sum16(v, v);
+    return v;
 }
 
-template <class T, int NS, int TPB, int KB>
-__global__ __launch_bounds__(TPB) void scan_bwd_kernel(ScanP P) {
-    constexpr int WAVES = TPB / 64, NV = 2 * NS;
-    __shared__ __attribute__((aligned(16))) float bc[KB * NV];
-    __shared__ float red[WAVES][KB][NV];
-    const int slot = (int)(blockIdx.x / (P.nblk * P.groups));
-    const int blk = (int)(blockIdx.x % (P.nblk * P.groups));
-    const Place q = place<TPB>(P, blk);
-    const int c = q.c, lane = (int)(threadIdx.x & 63), wave = (int)(threadIdx.x >> 6);
+template <class T, int NL, int LP, int KB>
+__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2, 2))) void scan_bwd_kernel(ScanP P) {
+    constexpr int NS = NL * LP;
+    __shared__ __attribute__((aligned(16))) float bc[KB * 2 * NS];
+    const Place q = place<LP>(P);
+    const int c = q.c, lane = (int)threadIdx.x, n0 = q.part * NL;
     const int64_t blocks = (P.length + KB - 1) / KB;
-    float a2[NS], dA[NS];
-    load_a2<NS>(P, c, a2);
+    float a2[NL], dA[NL];
+    {
+        const int k = states_here(P);
 #pragma unroll
-    for (int n = 0; n < NS; ++n) dA[n] = 0.f;
+        for (int n = 0; n < NL; ++n) {
+            a2[n] = n0 + n < k ? P.A[(int64_t)c * k + n0 + n] * kLog2e : 0.f;
+            dA[n] = 0.f;
+        }
+    }
+    const unsigned at_n = (unsigned)(n0 * P.channels + c);  // of the lane's first state in a row of states
     const float bias = P.bias ? P.bias[c] : 0.f, dd = P.D ? P.D[c] : 0.f;
     float dD = 0.f, dbias = 0.f;
-    for (int64_t job = slot; job < P.batch * P.chunks; job += P.slots) {
-        const int64_t b = job / P.chunks;
-        const int ch = (int)(job - b * P.chunks);
-        const int len = levels(P.lengths, b, P.length);
-        const int t0 = ch * P.chunk, tn = t0 + P.chunk < P.length ? t0 + P.chunk : P.length;
-        const int t1 = tn < len ? tn : len;
-        float G[NS];  // a_{t+1} g_{t+1} (0 with dy in idle lanes: they add nothing to dB and dC)
-        const float* ge = P.gend + job * P.states * P.channels + c;
+    auto states = [&](float (&h)[NL], const float* p) {
 #pragma unroll
-        for (int n = 0; n < NS; ++n)
-            G[n] = P.chunks > 1 && q.live && n < P.states ? ge[(int64_t)n * P.channels] : 0.f;
-        const int64_t row = b * P.length;
-        for (int t = t0 + (t1 - t0 - 1) / KB * KB; t1 > t0 && t >= t0; t -= KB) {
-            float h[NS], p[KB][NS];
-            float u[KB], raw[KB], dts[KB], dy[KB];
-            T rz[KB], ry[KB];
+        for (int n = 0; n < NL; ++n, p += P.channels) h[n] = p[at_n];
+    };
+    for (int64_t i = q.row; i < P.jobs; i += P.rows) {
+        const Job J = job_of(P, i);
+        float G[NL];  // a_{t+1} g_{t+1}
+        if (P.chunks > 1) {
+            states(G, P.gend + i * NS * P.channels);
+        } else {
 #pragma unroll
-            for (int j = 0; j < KB; ++j) {
-                const int s = t + j < t1 ? t + j : t1 - 1;
-                u[j] = to_f32<T>(at<T>(P.u, b, s, c));
-                raw[j] = to_f32<T>(at<T>(P.delta, b, s, c)) + bias;
-                ry[j] = at<T>(P.dy, b, s, c);
-                if (P.z.p) rz[j] = at<T>(P.z, b, s, c);
+            for (int n = 0; n < NL; ++n) G[n] = 0.f;
+        }
+        const int64_t row = J.b * P.length;
+        Tile<T, NS, KB> tile;
+        if (J.t0 < J.t1) tile.load(P, J.b, q.g, J.t0 + (J.t1 - J.t0 - 1) / KB * KB, J.t1);
+#pragma unroll 1
+        for (int t = J.t0 + (J.t1 - J.t0 - 1) / KB * KB; J.t1 > J.t0 && t >= J.t0; t -= KB) {
+            const ScanP Q = args_again();
+            Block<T, KB> raws;
+            {
+                Cursors<T> in;
+                in.set(Q, J.b, t, true, true);
+                in.load(raws, t, J.t1, c);
             }
-            const float* ck = P.ck + (b * blocks + t / KB) * P.states * P.channels;
+            float h[NL];
+            const int64_t k = J.b * blocks + t / KB;
+            states(h, Q.ck + k * NS * P.channels);
+            if (P.chunks > 1) {
+                // the state that the chunk starts from, decayed to the block
+                const float sum = (Q.cs + k * P.channels)[(unsigned)c];
+                float hc[NL];
+                states(hc, Q.hend + i * NS * P.channels);
 #pragma unroll
-            for (int n = 0; n < NS; ++n) h[n] = n < P.states ? (ck + (int64_t)n * P.channels)[(unsigned)c] : 0.f;
-            __syncthreads();
-            stage_bc<T, NS, TPB, KB, true>(P, b, q.g, t, t1, bc);
-            __syncthreads();
-#pragma unroll
-            for (int j = 0; j < KB; ++j) {
-                if (t + j >= t1) break;
-                const float* w = bc + j * NV;
-                dts[j] = P.softplus ? softplus(raw[j]) : raw[j];
+                for (int n = 0; n < NL; ++n)
+                    h[n] = fmaf(sum == 0.f ? 1.f : __builtin_amdgcn_exp2f(sum * a2[n]), hc[n], h[n]);
+            }
+            tile.store(Q, bc);
+            if (t > J.t0) tile.load(Q, J.b, q.g, t - KB, J.t1);
+            const int64_t r0 = (row + t) * P.channels;
+            float p[KB][NL], u[KB], raw[KB], dts[KB], dy[KB];
+            const int m = J.t1 - t;
+            T* dz_out = (T*)Q.dz + r0;
+            guarded<KB>(m, [&](int j) {
+                const Row<NS> w = row_of<NS>(bc, j, n0);
+                u[j] = to_f32<T>(raws.u[j]);
+                raw[j] = to_f32<T>(raws.d[j]) + bias;
+                dts[j] = step_of(P, raw[j]);
                 const float du = dts[j] * u[j];
                 float y = 0.f;
 #pragma unroll
-                for (int n = 0; n < NS; ++n) {
+                for (int n = 0; n < NL; ++n) {
                     p[j][n] = __builtin_amdgcn_exp2f(dts[j] * a2[n]) * h[n];
                     h[n] = fmaf(du, w[n], p[j][n]);
                     y = fmaf(h[n], w[NS + n], y);
                 }
-                dy[j] = q.live ? to_f32<T>(ry[j]) : 0.f;
-                if (P.z.p) {
-                    const float z = to_f32<T>(rz[j]), s = sigmoid(z), dz = dy[j] * fmaf(dd, u[j], y);
-                    if (q.live) put<T>(P.dz, row + t + j, P.channels, c, dz * (s * fmaf(z, 1.f - s, 1.f)));
-                    dy[j] *= z * s;
-                }
-                __builtin_amdgcn_sched_barrier(0);
-            }
-#pragma unroll
-            for (int j = KB - 1; j >= 0; --j) {
-                if (t + j >= t1) continue;
-                const float* w = bc + j * NV;
+                y = fmaf(dd, u[j], parts_sum<LP>(y));
+                const float dout = to_f32<T>(raws.g[j]), z = to_f32<T>(raws.z[j]), s = sigmoid(z);
+                dy[j] = P.gate ? dout * (z * s) : dout;
+                // (a channel's lanes store the same value)
+                if (P.gate) dz_out[(unsigned)c] = from_f32<T>(dout * y * (s * fmaf(z, 1.f - s, 1.f)));
+                dz_out += P.channels;
+                level_fence();
+            });
+            // back from the block's last level
+            const int last = m < KB ? m - 1 : KB - 1;
+            const ScanP R = args_again();
+            T* du_out = (T*)R.y + r0 + (int64_t)last * P.channels;
+            T* dd_out = (T*)R.ddelta + r0 + (int64_t)last * P.channels;
+            float* bc_out = R.pbc + (((int64_t)q.blk * P.batch + J.b) * P.length + t + last) * (2 * NS);
+            back_guarded<KB>(m, [&](int j) {
+                const Row<NS> w = row_of<NS>(bc, j, n0);
                 // a_t and h_t are formed again, not kept: with them the block would not fit the registers
                 float dt = dts[j];
                 asm volatile("" : "+v"(dt));
-                const float du = dt * u[j];
-                float v[NS], gB = 0.f, gA = 0.f;
+                const float du = dt * u[j], dul = q.live ? du : 0.f, dyl = q.live ? dy[j] : 0.f;
+                float v[NL], gB = 0.f, gA = 0.f;
 #pragma unroll
-                for (int n = 0; n < NS; ++n) v[n] = fmaf(du, w[n], p[j][n]) * dy[j];
-                const float sc = reduce_lanes<NS>(v);
+                for (int n = 0; n < NL; ++n) v[n] = fmaf(du, w[n], p[j][n]) * dyl;
+                const float sc = reduce_lanes<NL, LP>(v);
 #pragma unroll
-                for (int n = 0; n < NS; ++n) {
+                for (int n = 0; n < NL; ++n) {
                     const float g = fmaf(w[NS + n], dy[j], G[n]);
                     const float gp = g * p[j][n];
-                    v[n] = g * du;
+                    v[n] = g * dul;
                     gB = fmaf(g, w[n], gB);
                     gA = fmaf(gp, a2[n], gA);
                     dA[n] = fmaf(dt, gp, dA[n]);
                     G[n] = __builtin_amdgcn_exp2f(dt * a2[n]) * g;
                 }
-                const float sb = reduce_lanes<NS>(v);
+                const float sb = reduce_lanes<NL, LP>(v);
+                gB = parts_sum<LP>(gB), gA = parts_sum<LP>(gA);
                 float dl = fmaf(gA, kLn2, gB * u[j]);
-                if (P.softplus) dl *= sigmoid(raw[j]);
+                const float slope = sigmoid(raw[j]);
+                dl = P.softplus ? dl * slope : dl;
                 dD = fmaf(dy[j], u[j], dD);
                 dbias += dl;
-                if (q.live) {
-                    put<T>(P.y, row + t + j, P.channels, c, fmaf(dt, gB, dd * dy[j]));
-                    put<T>(P.ddelta, row + t + j, P.channels, c, dl);
-                }
-                if (lane % (64 / NS) == 0) {
-                    red[wave][j][lane / (64 / NS)] = sb;
-                    red[wave][j][NS + lane / (64 / NS)] = sc;
-                }
-                __builtin_amdgcn_sched_barrier(0);  // (one level's values at a time)
-            }
-            __syncthreads();
-            // the workgroup's sums of this block
-            const int m = (t1 - t < KB ? t1 - t : KB) * NV;
-            float* out = P.pbc + (((int64_t)blk * P.batch + b) * P.length + t) * NV;
-            for (int e = (int)threadIdx.x; e < m; e += TPB) {
-                float s = red[0][e / NV][e % NV];
-#pragma unroll
-                for (int k = 1; k < WAVES; ++k) s += red[k][e / NV][e % NV];
-                out[e] = s;
-            }
+                du_out[(unsigned)c] = from_f32<T>(fmaf(dt, gB, dd * dy[j]));
+                dd_out[(unsigned)c] = from_f32<T>(dl);
+                du_out -= P.channels, dd_out -= P.channels;
+                // value n of both sums is in L lanes of the part's
+                constexpr int L = 64 / NS;
+                if (lane % L < 2) bc_out[(unsigned)(lane / L + lane % L * NS)] = lane % L ? sc : sb;
+                bc_out -= 2 * NS;
+                level_fence();
+            });
         }
-        if (q.live)
-            for (int t = t1 > t0 ? t1 : t0; t < tn; ++t) {
-                put<T>(P.y, row + t, P.channels, c, 0.f);
-                put<T>(P.ddelta, row + t, P.channels, c, 0.f);
-                if (P.z.p) put<T>(P.dz, row + t, P.channels, c, 0.f);
-            }
+        for (int t = J.t1 > J.t0 ? J.t1 : J.t0; t < J.tn; ++t) {
+            put<T>(P.y, row + t, P.channels, c, 0.f);
+            put<T>(P.ddelta, row + t, P.channels, c, 0.f);
+            if (P.gate) put<T>(P.dz, row + t, P.channels, c, 0.f);
+        }
     }
     if (!q.live) return;
-    float* s = P.pA + ((int64_t)slot * P.channels + c) * P.states;
+    const int k = states_here(P);
+    float* s = P.pA + ((int64_t)q.row * P.channels + c) * k + n0;
 #pragma unroll
-    for (int n = 0; n < NS; ++n)
-        if (n < P.states) s[n] = dA[n];
-    if (P.pD) P.pD[(int64_t)slot * P.channels + c] = dD;
-    if (P.pbias) P.pbias[(int64_t)slot * P.channels + c] = dbias;
+    for (int n = 0; n < NL; ++n)
+        if (n0 + n < k) s[n] = dA[n];
+    if (P.pD) P.pD[(int64_t)q.row * P.channels * 2 + c] = dD;
+    if (P.pbias) P.pbias[(int64_t)q.row * P.channels * 2 + c] = dbias;
 }
 
-// dB and dC from the workgroups' partial sums: one lane a (level, group, n, which).
+// dB and dC from the wavefronts' partial sums: one lane a (level, group, n, which).
 template <class T>
 __global__ __launch_bounds__(256) void scan_bc_kernel(ScanP P, int ns, T* dB, T* dC) {
     const int per = P.groups * 2 * ns;
@@ -553,37 +816,42 @@ __global__ __launch_bounds__(256) void scan_bc_kernel(ScanP P, int ns, T* dB, T*
 
 constexpr int64_t kMaxChannels = 1 << 20, kMaxLevels = (int64_t)1 << 40;
 
-int lanes_of(int64_t per) { return per <= 64 ? 64 : per <= 128 ? 128 : 256; }
 int states_of(int states) { return states <= 4 ? 4 : states <= 8 ? 8 : states <= 16 ? 16 : 32; }
-int block_of(int ns) { return ns == 32 ? 4 : 8; }
+constexpr int kBlock = 8;  // levels between saved states in the backward
+// lanes of a channel in the backward's main pass
+int parts_of(int ns) { return ns <= 8 ? 1 : ns / 8; }
 
 struct Plan {
-    int tpb, nblk, per, ns, chunk, chunks, slots;
+    int nblk, per, ns, chunk, chunks;
+    int64_t jobs;
+    int rows, bwd_rows, bwd_nblk;
 };
 
 // Wavefronts that fill the card: one for each SIMD.  Whole windows with fewer are
-// split in chunks, as long as a chunk keeps kMinChunk levels.
-constexpr int64_t kFill = 1024;
-constexpr int kMinChunk = 64;
-// Workgroup rows of partial dA sums.
-constexpr int64_t kSlots = 2048;
+// split in chunks until there are kWaves, as long as a chunk keeps kMinChunk levels.
+constexpr int64_t kFill = 1024, kWaves = 4096;
+constexpr int kMinChunk = 32;
+// Most wavefronts of a launch; of the backward's main launch, whose partial sums of dA grow with them.
+constexpr int64_t kMaxWaves = (int64_t)1 << 24, kBwdWaves = 8192;
 
 Plan plan(int64_t batch, int64_t length, int64_t channels, int states, int groups) {
     Plan p;
     p.per = (int)(channels / groups);
-    p.tpb = lanes_of(p.per);
-    p.nblk = (int)cdiv(p.per, p.tpb);
+    p.nblk = (int)cdiv(p.per, 64);
     p.ns = states_of(states);
-    const int64_t waves = (batch < 1 ? 1 : batch) * groups * p.nblk * (p.tpb / 64);
-    int64_t n = waves >= kFill ? 1 : cdiv(2 * kFill, waves);
+    const int64_t row = (int64_t)groups * p.nblk, waves = (batch < 1 ? 1 : batch) * row;
+    int64_t n = waves >= kFill ? 1 : cdiv(kWaves, waves);
     const int64_t most = length / kMinChunk;
     if (n > most) n = most < 1 ? 1 : most;
-    p.chunk = (int)(cdiv(cdiv(length < 1 ? 1 : length, n), kTile) * kTile);
+    p.chunk = (int)(cdiv(cdiv(length < 1 ? 1 : length, n), 8) * 8);
     p.chunks = (int)cdiv(length < 1 ? 1 : length, p.chunk);
-    const int64_t jobs = batch * p.chunks, wg = (int64_t)groups * p.nblk;
-    int64_t s = kSlots / wg;
-    if (s < 64) s = 64;
-    p.slots = (int)(jobs < s ? (jobs < 1 ? 1 : jobs) : s);
+    p.jobs = batch * p.chunks;
+    auto rows = [&](int64_t most_waves, int nblk) {
+        const int64_t r = most_waves / ((int64_t)groups * nblk);
+        return (int)(p.jobs < 1 ? 1 : (r < 1 ? 1 : (p.jobs < r ? p.jobs : r)));
+    };
+    p.bwd_nblk = (int)cdiv(p.per, 64 / parts_of(p.ns));
+    p.rows = rows(kMaxWaves, p.nblk), p.bwd_rows = rows(kBwdWaves, p.bwd_nblk);
     return p;
 }
 
@@ -595,8 +863,6 @@ int check_scan(int dtype, int states, int groups, int sp, int64_t batch, int64_t
         return FPDE_ERR_SHAPE;
     if (states > 32) return FPDE_ERR_UNSUPPORTED;
     if (batch > kMaxLevels || (length > 0 && batch > kMaxLevels / length)) return FPDE_ERR_SHAPE;
-    const Plan p = plan(batch, length, channels, states, groups);
-    if (batch * p.chunks > (((int64_t)1 << 31) - 1) / ((int64_t)p.nblk * groups * p.tpb)) return FPDE_ERR_SHAPE;
     return FPDE_OK;
 }
 
@@ -606,22 +872,15 @@ bool seq_ok(const Seq& s, int64_t batch, int64_t length, int64_t width) {
     return batch <= 1 || (s.bs >= 0 && s.bs <= most / batch);
 }
 
-// f(T{}, NS, TPB)
+// f(T{}, NS)
 template <class F>
 int with_scan(int dtype, const Plan& p, F f) {
     return with_type(dtype, [&](auto t) {
-        auto wg = [&](auto ns) {
-            switch (p.tpb) {
-            case 64: return f(t, ns, std::integral_constant<int, 64>{});
-            case 128: return f(t, ns, std::integral_constant<int, 128>{});
-            default: return f(t, ns, std::integral_constant<int, 256>{});
-            }
-        };
         switch (p.ns) {
-        case 4: return wg(std::integral_constant<int, 4>{});
-        case 8: return wg(std::integral_constant<int, 8>{});
-        case 16: return wg(std::integral_constant<int, 16>{});
-        default: return wg(std::integral_constant<int, 32>{});
+        case 4: return f(t, std::integral_constant<int, 4>{});
+        case 8: return f(t, std::integral_constant<int, 8>{});
+        case 16: return f(t, std::integral_constant<int, 16>{});
+        default: return f(t, std::integral_constant<int, 32>{});
         }
     });
 }
@@ -631,13 +890,14 @@ ScanP params(const A* a, const Plan& p) {
     ScanP P{};
     P.u = Seq{a->u, a->u_batch_stride, a->u_time_stride};
     P.delta = Seq{a->delta, a->delta_batch_stride, a->delta_time_stride};
-    P.z = Seq{a->z, a->z_batch_stride, a->z_time_stride};
+    P.z = a->z ? Seq{a->z, a->z_batch_stride, a->z_time_stride} : P.u;
+    P.gate = a->z != nullptr;
     P.B = Seq{a->B, a->b_batch_stride, a->b_time_stride};
     P.C = Seq{a->C, a->c_batch_stride, a->c_time_stride};
     P.A = a->A, P.D = a->D, P.bias = a->delta_bias, P.state = a->state, P.lengths = a->lengths;
     P.batch = a->batch, P.length = (int)a->length, P.channels = (int)a->channels;
     P.states = a->states, P.groups = a->groups, P.softplus = a->softplus;
-    P.chunk = p.chunk, P.chunks = p.chunks, P.per = p.per, P.nblk = p.nblk, P.slots = p.slots;
+    P.chunk = p.chunk, P.chunks = p.chunks, P.per = p.per, P.nblk = p.nblk, P.jobs = p.jobs, P.rows = p.rows;
     return P;
 }
 
@@ -660,41 +920,44 @@ int check_inputs(const A* a, const ScanP& P, Spans* sp) {
     return FPDE_OK;
 }
 
-unsigned grid_of(const ScanP& P, int64_t rows) { return (unsigned)(rows * P.nblk * P.groups); }
+dim3 grid_of(const ScanP& P) { return dim3((unsigned)((int64_t)P.rows * P.nblk * P.groups)); }
 
-int queue_chunks(const ScanP& P, float* e, int backward, hipStream_t s) {
-    const dim3 g((unsigned)cdiv(P.channels, 256), (unsigned)P.states,
-                 (unsigned)(P.batch < 65535 ? P.batch : 65535));
-    return launch(chunk_kernel, g, dim3(256), s, P, e, backward);
+// the scan over chunks of e, and of e2 for the adjoint
+int queue_chunks(const ScanP& P, int ns, float* e, float* e2, hipStream_t s) {
+    const int64_t most = 65535 / P.states;
+    const dim3 g((unsigned)cdiv(P.channels, 64), (unsigned)((P.batch < most ? P.batch : most) * P.states), e2 ? 2 : 1);
+    const int64_t waves = cdiv(P.chunks, 32);
+    return launch(chunk_kernel, g, dim3((unsigned)(waves < 8 ? waves : 8) * 64), s, P, ns, e, e2);
 }
 
-// floats of one [batch][chunks][states][channels] array and of the sums of dt
-int64_t ends_of(int64_t batch, int64_t channels, int states, const Plan& p) {
-    return p.chunks > 1 ? batch * p.chunks * states * channels : 0;
-}
-int64_t sums_of(int64_t batch, int64_t channels, const Plan& p) {
-    return p.chunks > 1 ? batch * p.chunks * channels : 0;
-}
-
-struct BwdSpace {
-    int64_t hend, gend, sdt, ck, pbc, pA, pD, total;
-};
-BwdSpace bwd_space(int64_t batch, int64_t length, int64_t channels, int states, int groups, const Plan& p) {
-    BwdSpace w;
-    int64_t n = 0;
-    auto take = [&](int64_t k) {
-        const int64_t at = n;
-        n += (k + 3) / 4 * 4;
+// The workspaces, in floats: offsets of their parts.
+struct Space {
+    int64_t hend = 0, gend = 0, sdt = 0, ck = 0, cs = 0, pbc = 0, pA = 0, pD = 0, total = 0;
+    int64_t take(int64_t k) {
+        const int64_t at = total;
+        total += (k + 3) / 4 * 4;
         return at;
-    };
-    w.hend = take(ends_of(batch, channels, states, p));
-    w.gend = take(ends_of(batch, channels, states, p));
-    w.sdt = take(sums_of(batch, channels, p));
-    w.ck = take(batch * cdiv(length, block_of(p.ns)) * states * channels);
-    w.pbc = take((int64_t)groups * p.nblk * batch * length * 2 * p.ns);
-    w.pA = take((int64_t)p.slots * channels * states);
-    w.pD = take((int64_t)p.slots * channels * 2);
-    w.total = n * 4;
+    }
+};
+Space fwd_space(int64_t batch, int64_t length, int64_t channels, int groups, const Plan& p) {
+    Space w;
+    if (p.chunks > 1) {
+        w.hend = w.take(p.jobs * p.ns * channels);
+        w.sdt = w.take(p.jobs * channels);
+    }
+    return w;
+}
+Space bwd_space(int64_t batch, int64_t length, int64_t channels, int states, int groups, const Plan& p) {
+    Space w = fwd_space(batch, length, channels, groups, p);
+    const int64_t blocks = batch * cdiv(length, kBlock);
+    if (p.chunks > 1) {
+        w.gend = w.take(p.jobs * p.ns * channels);
+        w.cs = w.take(blocks * channels);
+    }
+    w.ck = w.take(blocks * p.ns * channels);
+    w.pbc = w.take((int64_t)groups * p.bwd_nblk * batch * length * 2 * p.ns);
+    w.pA = w.take((int64_t)p.bwd_rows * channels * states);
+    w.pD = w.take((int64_t)p.bwd_rows * channels * 2);
     return w;
 }
 
@@ -704,8 +967,9 @@ extern "C" int64_t fpde_selective_scan_workspace(const fpde_scan_args* a) {
     if (!a) return FPDE_ERR_ARG;
     const int st = check_scan(a->dtype, a->states, a->groups, a->softplus, a->batch, a->length, a->channels);
     if (st != FPDE_OK) return st;
+    if (a->length <= 1) return 0;
     const Plan p = plan(a->batch, a->length, a->channels, a->states, a->groups);
-    return (ends_of(a->batch, a->channels, a->states, p) + sums_of(a->batch, a->channels, p)) * 4;
+    return fwd_space(a->batch, a->length, a->channels, a->groups, p).total * 4;
 }
 
 extern "C" int fpde_selective_scan(const fpde_scan_args* a, void* stream) {
@@ -725,24 +989,24 @@ extern "C" int fpde_selective_scan(const fpde_scan_args* a, void* stream) {
     if (st != FPDE_OK) return st;
     if (a->batch == 0 || (a->length == 0 && !a->state_out)) return FPDE_OK;
     P.y = a->y, P.state_out = a->state_out;
-    P.hend = (float*)a->workspace;
-    if (need > 0) P.sdt = P.hend + ends_of(a->batch, a->channels, a->states, p);
+    const Space w = fwd_space(a->batch, a->length, a->channels, a->groups, p);
+    float* ws = (float*)a->workspace;
+    P.hend = ws + w.hend, P.sdt = ws + w.sdt;
     hipStream_t s = (hipStream_t)stream;
-    return with_scan(a->dtype, p, [&](auto t, auto nsc, auto tpbc) {
+    return with_scan(a->dtype, p, [&](auto t, auto nsc) {
         using T = decltype(t);
-        constexpr int NS = decltype(nsc)::value, TPB = decltype(tpbc)::value;
+        constexpr int NS = decltype(nsc)::value;
         if (a->length == 1) {
             const dim3 g((unsigned)cdiv(a->channels * (NS / 4), 256),
                          (unsigned)(a->batch < 65535 ? a->batch : 65535));
             return launch(scan_step_kernel<T, NS>, g, dim3(256), s, P);
         }
-        const dim3 g(grid_of(P, a->batch * P.chunks));
+        int r = FPDE_OK;
         if (P.chunks > 1) {
-            int r = launch(scan_fwd_kernel<T, NS, TPB, ENDS, 8>, g, dim3(TPB), s, P);
-            if (r == FPDE_OK) r = queue_chunks(P, P.hend, 0, s);
-            if (r != FPDE_OK) return r;
+            r = launch(scan_fwd_kernel<T, NS, false>, grid_of(P), dim3(64), s, P);
+            if (r == FPDE_OK) r = queue_chunks(P, NS, P.hend, nullptr, s);
         }
-        return launch(scan_fwd_kernel<T, NS, TPB, OUT, 8>, g, dim3(TPB), s, P);
+        return r != FPDE_OK ? r : launch(scan_fwd_kernel<T, NS, true>, grid_of(P), dim3(64), s, P);
     });
 }
 
@@ -751,7 +1015,7 @@ extern "C" int64_t fpde_selective_scan_bwd_workspace(const fpde_scan_bwd_args* a
     const int st = check_scan(a->dtype, a->states, a->groups, a->softplus, a->batch, a->length, a->channels);
     if (st != FPDE_OK) return st;
     const Plan p = plan(a->batch, a->length, a->channels, a->states, a->groups);
-    return bwd_space(a->batch, a->length, a->channels, a->states, a->groups, p).total;
+    return bwd_space(a->batch, a->length, a->channels, a->states, a->groups, p).total * 4;
 }
 
 extern "C" int fpde_selective_scan_bwd(const fpde_scan_bwd_args* a, void* stream) {
@@ -784,29 +1048,27 @@ extern "C" int fpde_selective_scan_bwd(const fpde_scan_bwd_args* a, void* stream
     sp.add(a->workspace, need, 16, true);
     st = sp.check();
     if (st != FPDE_OK) return st;
-    const BwdSpace w = bwd_space(a->batch, a->length, a->channels, a->states, a->groups, p);
+    const Space w = bwd_space(a->batch, a->length, a->channels, a->states, a->groups, p);
     float* ws = (float*)a->workspace;
-    P.hend = ws + w.hend, P.gend = ws + w.gend, P.sdt = ws + w.sdt, P.ck = ws + w.ck, P.pbc = ws + w.pbc;
-    P.pA = ws + w.pA;
+    P.hend = ws + w.hend, P.gend = ws + w.gend, P.sdt = ws + w.sdt;
+    P.ck = ws + w.ck, P.cs = ws + w.cs, P.pbc = ws + w.pbc, P.pA = ws + w.pA;
     P.pD = a->D ? ws + w.pD : nullptr;
-    P.pbias = a->delta_bias ? ws + w.pD + (int64_t)p.slots * a->channels : nullptr;
+    P.pbias = a->delta_bias ? ws + w.pD + a->channels : nullptr;
     P.y = a->du, P.ddelta = a->ddelta, P.dz = a->dz;
     hipStream_t s = (hipStream_t)stream;
     if (n > 0) {
-        st = with_scan(a->dtype, p, [&](auto t, auto nsc, auto tpbc) {
+        st = with_scan(a->dtype, p, [&](auto t, auto nsc) {
             using T = decltype(t);
-            constexpr int NS = decltype(nsc)::value, TPB = decltype(tpbc)::value, KB = NS == 32 ? 4 : 8;
-            const dim3 g(grid_of(P, a->batch * P.chunks));
-            int r = FPDE_OK;
+            constexpr int NS = decltype(nsc)::value, KB = kBlock, LP = NS <= 8 ? 1 : NS / 8;
+            int r;
             if (P.chunks > 1) {
-                r = launch(scan_fwd_kernel<T, NS, TPB, ENDS, KB>, g, dim3(TPB), s, P);
-                if (r == FPDE_OK) r = launch(scan_adj_kernel<T, NS, TPB>, g, dim3(TPB), s, P);
-                if (r == FPDE_OK) r = queue_chunks(P, P.hend, 0, s);
-                if (r == FPDE_OK) r = queue_chunks(P, P.gend, 1, s);
+                r = launch(scan_pre_kernel<T, NS, KB, true>, grid_of(P), dim3(64), s, P);
+                if (r == FPDE_OK) r = queue_chunks(P, NS, P.hend, P.gend, s);
+            } else {
+                r = launch(scan_pre_kernel<T, NS, KB, false>, grid_of(P), dim3(64), s, P);
             }
-            if (r == FPDE_OK) r = launch(scan_fwd_kernel<T, NS, TPB, CHECKS, KB>, g, dim3(TPB), s, P);
-            if (r == FPDE_OK)
-                r = launch(scan_bwd_kernel<T, NS, TPB, KB>, dim3(grid_of(P, P.slots)), dim3(TPB), s, P);
+            P.rows = p.bwd_rows, P.nblk = p.bwd_nblk;
+            if (r == FPDE_OK) r = launch(scan_bwd_kernel<T, NS / LP, LP, KB>, grid_of(P), dim3(64), s, P);
             if (r != FPDE_OK) return r;
             const int64_t bcs = cdiv(n * a->groups * 2 * NS, 256);
             return launch(scan_bc_kernel<T>, dim3((unsigned)(bcs < 65536 ? bcs : 65536)), dim3(256), s, P, NS,
@@ -814,11 +1076,13 @@ extern "C" int fpde_selective_scan_bwd(const fpde_scan_bwd_args* a, void* stream
         });
         if (st != FPDE_OK) return st;
     }
-    const int64_t rows = n > 0 ? p.slots : 0, cols = a->channels * a->states;
+    const int64_t rows = n > 0 ? p.bwd_rows : 0, cols = a->channels * a->states, two = a->channels * 2;
     st = queue_colsum(P.pA, rows, cols, a->dA, cols, nullptr, 0, FPDE_F32, s);
-    if (st == FPDE_OK && P.pD)
-        st = queue_colsum(P.pD, rows, a->channels, a->dD, a->channels, nullptr, 0, FPDE_F32, s);
-    if (st == FPDE_OK && P.pbias)
-        st = queue_colsum(P.pbias, rows, a->channels, a->ddelta_bias, a->channels, nullptr, 0, FPDE_F32, s);
+    if (st == FPDE_OK && (P.pD || P.pbias)) {
+        // (side by side in one partial row)
+        float* first = P.pD ? P.pD : P.pbias;
+        st = queue_colsum(first, rows, two, P.pD ? a->dD : a->ddelta_bias, a->channels, a->ddelta_bias,
+                          P.pD && P.pbias ? a->channels : 0, FPDE_F32, s);
+    }
     return st;
 }
