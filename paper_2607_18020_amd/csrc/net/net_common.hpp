@@ -114,10 +114,11 @@ __device__ __forceinline__ float param(const void* p, bool f32, int64_t at) {
 // Cross-lane sums and maxima over groups of LANES (a power of two, at most 64)
 // neighbouring lanes; every lane gets the result.
 
+// (every lane has a source: with bound_ctrl set the move becomes part of the instruction that uses it)
 template <int CTRL>
 __device__ __forceinline__ float dpp(float v) {
     return __builtin_bit_cast(
-        float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, false));
+        float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
 }
 
 struct AddOp {

@@ -36,15 +36,30 @@ namespace {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr float kS = 4096.f, kInvS = 1.f / 4096.f, kInvSS = kInvS * kInvS;
 
-__device__ __forceinline__ void split(float v, f16& hi, f16& lo) {
-    const float t = v * kS;
-    hi = (f16)t;
-    lo = (f16)(t - (float)hi);
+// Values that carry the factor S already, in pairs: hi and lo.  (Two conversions, two differences and
+// two conversions back for a pair: the small kernel spends as much on this as on its products.)
+__device__ __forceinline__ void split2(float a, float b, f16x2& hi, f16x2& lo) {
+    const f32x2 t = {a, b};
+    hi = __builtin_convertvector(t, f16x2);
+    const f32x2 r = {a - (float)hi[0], b - (float)hi[1]};
+    lo = __builtin_convertvector(r, f16x2);
+}
+template <int N, class H>
+__device__ __forceinline__ void split(const float (&v)[N], H& hi, H& lo) {
+#pragma unroll
+    for (int e = 0; e < N; e += 2) {
+        f16x2 h, l;
+        split2(v[e], v[e + 1], h, l);
+        hi[e] = h[0], hi[e + 1] = h[1];
+        lo[e] = l[0], lo[e + 1] = l[1];
+    }
 }
 
 constexpr int kMaxCount = 32;  // matrices of one launch
@@ -96,28 +111,36 @@ __device__ __forceinline__ float inv_norm(double sumsq, float eps) {
 // ---------------------------------------------------------------------------
 // Small matrices.
 
-// Products of rows of U and rows of V, both [rows][pitch] in LDS, hi then lo `half`
-// elements later: MT x NT tiles of 16 x 16.  A lane reads 8 neighbouring k of row l % 16.
-template <int MT, int NT>
+// Products of rows of U and rows of V, both [rows][pitch] in LDS, hi then lo `hu`, `hv` elements
+// later: MT x NT tiles of 16 x 16.  A lane reads 8 neighbouring k of row l % 16; the next 32 k are
+// read while these are multiplied.
+template <int MT, int NT, int K>
 __device__ __forceinline__ void lds_product(f32x4 (&acc)[MT][NT], const f16* U, int pu, int hu, const f16* V,
-                                            int pv, int hv, int K) {
+                                            int pv, int hv) {
     const int lane = (int)(threadIdx.x & 63), r = lane & 15, k0 = (lane >> 4) * 8;
+    U += r * pu + k0, V += r * pv + k0;
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int k = k0; k < K; k += 32) {
-        f16x8 uh[MT], ul[MT], vh[NT], vl[NT];
-#pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            uh[i] = *(const f16x8*)(U + (i * 16 + r) * pu + k);
-            ul[i] = *(const f16x8*)(U + hu + (i * 16 + r) * pu + k);
-        }
+    f16x8 uh[2][MT], ul[2][MT], vh[2][NT], vl[2][NT];
+    auto read = [&](int b, int k) {
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-            vh[j] = *(const f16x8*)(V + (j * 16 + r) * pv + k);
-            vl[j] = *(const f16x8*)(V + hv + (j * 16 + r) * pv + k);
+            vl[b][j] = *(const f16x8*)(V + hv + j * 16 * pv + k);
+            vh[b][j] = *(const f16x8*)(V + j * 16 * pv + k);
         }
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            uh[b][i] = *(const f16x8*)(U + i * 16 * pu + k);
+            ul[b][i] = *(const f16x8*)(U + hu + i * 16 * pu + k);
+        }
+    };
+    read(0, 0);
+#pragma unroll
+    for (int k = 0; k < K; k += 32) {
+        const int b = k / 32 & 1;
+        if (k + 32 < K) read(b ^ 1, k + 32);
         // (a sum's three products are apart, so that none waits for the one before)
 #pragma unroll
         for (int p = 0; p < 3; ++p)
@@ -125,23 +148,42 @@ __device__ __forceinline__ void lds_product(f32x4 (&acc)[MT][NT], const f16* U, 
             for (int i = 0; i < MT; ++i)
 #pragma unroll
                 for (int j = 0; j < NT; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p == 1 ? ul[i] : uh[i], p ? vh[j] : vl[j],
-                                                                       acc[i][j], 0, 0, 0);
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+                        p == 1 ? ul[b][i] : uh[b][i], p ? vh[b][j] : vl[b][j], acc[i][j], 0, 0, 0);
     }
 }
 
-// Four neighbouring k of row `row` (the four rows of one column of a result tile)
-__device__ __forceinline__ void put4(f16* p, int half, const float (&v)[4]) {
-    f16x4 h, l;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        f16 a, b;
-        split(v[e], a, b);
-        h[e] = a, l[e] = b;
+// hi and lo of four rows of one column of a result tile, as four neighbouring k
+struct Quad {
+    f16x4 hi, lo;
+    __device__ __forceinline__ explicit Quad(const float (&v)[4]) { split<4>(v, hi, lo); }
+    __device__ __forceinline__ void put(f16* p, int half) const {
+        *(f16x4*)p = hi;
+        *(f16x4*)(p + half) = lo;
     }
-    *(f16x4*)p = h;
-    *(f16x4*)(p + half) = l;
-}
+    // The same by rows, `pitch` apart, from p on.  Neighbouring lanes hold neighbouring columns; the even one
+    // takes the first two rows of both and the odd one the others, so that a write is two columns wide.
+    __device__ __forceinline__ void put_rows(f16* p, int pitch, int half) const {
+        const bool odd = threadIdx.x & 1;
+        p += odd ? 2 * pitch - 1 : 0;
+        two_rows(hi, p, pitch, odd);
+        two_rows(lo, p + half, pitch, odd);
+    }
+
+private:
+    static __device__ __forceinline__ void two_rows(const f16x4& v, f16* p, int pitch, bool odd) {
+        struct Words {
+            uint32_t a, b;
+        };
+        const Words w = __builtin_bit_cast(Words, v);  // rows 0, 1 and rows 2, 3
+        const uint32_t mine = odd ? w.b : w.a;
+        const uint32_t other = (uint32_t)__builtin_amdgcn_mov_dpp((int)(odd ? w.a : w.b), 0xB1, 0xF, 0xF, true);
+        const uint32_t even_col = odd ? other : mine, odd_col = odd ? mine : other;
+        // (byte selections: the low halves of both, the high halves of both)
+        *(uint32_t*)p = __builtin_amdgcn_perm(odd_col, even_col, 0x05040100);
+        *(uint32_t*)(p + pitch) = __builtin_amdgcn_perm(odd_col, even_col, 0x07060302);
+    }
+};
 
 // One workgroup of 8 wavefronts, 2 x 4 of them over the rows and columns of X, a matrix.
 template <class T, int SP, int LP>
@@ -205,32 +247,29 @@ __global__ __launch_bounds__(512) void ortho_small_kernel(Mats M, int steps, flo
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[i][j][e] *= inv;
+            for (int e = 0; e < 4; ++e) x[i][j][e] *= inv * kS;
+    // From here on x, A and B are S times what they stand for.
     for (int it = 0; it < steps; ++it) {
         // X by rows
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int j = 0; j < NT; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    f16* p = lds1 + (row0 + i * 16 + r4 + e) * PL + col0 + j * 16 + cl;
-                    split(x[i][j][e], p[0], p[R1]);
-                }
+                Quad(x[i][j]).put_rows(lds1 + (row0 + i * 16 + r4) * PL + col0 + j * 16 + cl, PL, R1);
         __syncthreads();
         f32x4 acc[MT][AT];
-        lds_product<MT, AT>(acc, lds1 + row0 * PL, PL, R1, lds1 + acol0 * PL, PL, R1, LP);
+        lds_product<MT, AT, LP>(acc, lds1 + row0 * PL, PL, R1, lds1 + acol0 * PL, PL, R1);
         float A[MT][AT][4];
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int j = 0; j < AT; ++j) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) A[i][j][e] = acc[i][j][e] * kInvSS;
-                put4(lds2 + (acol0 + j * 16 + cl) * PS + row0 + i * 16 + r4, R2, A[i][j]);  // (symmetric)
+                for (int e = 0; e < 4; ++e) A[i][j][e] = acc[i][j][e] * kInvS;
+                Quad(A[i][j]).put(lds2 + (acol0 + j * 16 + cl) * PS + row0 + i * 16 + r4, R2);  // (symmetric)
             }
         __syncthreads();
-        lds_product<MT, AT>(acc, lds2 + row0 * PS, PS, R2, lds2 + acol0 * PS, PS, R2, SP);
+        lds_product<MT, AT, SP>(acc, lds2 + row0 * PS, PS, R2, lds2 + acol0 * PS, PS, R2);
         // (every wavefront is past its reads of X by rows: B takes its place)
 #pragma unroll
         for (int i = 0; i < MT; ++i)
@@ -238,30 +277,31 @@ __global__ __launch_bounds__(512) void ortho_small_kernel(Mats M, int steps, flo
             for (int j = 0; j < AT; ++j) {
                 float b[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) b[e] = fmaf(cb, A[i][j][e], cc * kInvSS * acc[i][j][e]);
-                put4(lds1 + (acol0 + j * 16 + cl) * PS + row0 + i * 16 + r4, R1, b);
+                for (int e = 0; e < 4; ++e) b[e] = fmaf(cb, A[i][j][e], cc * kInvS * acc[i][j][e]);
+                Quad(b).put(lds1 + (acol0 + j * 16 + cl) * PS + row0 + i * 16 + r4, R1);
             }
         __syncthreads();  // (and past those of A: X by columns takes its place)
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int j = 0; j < NT; ++j)
-                put4(lds2 + (col0 + j * 16 + cl) * PS + row0 + i * 16 + r4, R2, x[i][j]);
+                Quad(x[i][j]).put(lds2 + (col0 + j * 16 + cl) * PS + row0 + i * 16 + r4, R2);
         __syncthreads();
         f32x4 y[MT][NT];
-        lds_product<MT, NT>(y, lds1 + row0 * PS, PS, R1, lds2 + col0 * PS, PS, R2, SP);
+        lds_product<MT, NT, SP>(y, lds1 + row0 * PS, PS, R1, lds2 + col0 * PS, PS, R2);
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int j = 0; j < NT; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[i][j][e] = fmaf(ca, x[i][j][e], y[i][j][e] * kInvSS);
+                for (int e = 0; e < 4; ++e) x[i][j][e] = fmaf(ca, x[i][j][e], y[i][j][e] * kInvS);
         __syncthreads();
     }
     T w[MT][NT][4];
     if (M.muon) each([&](int i, int j, int e, int64_t k, bool) { w[i][j][e] = ((const T*)M.out[mat])[k]; });
     each([&](int i, int j, int e, int64_t k, bool in) {
-        const float v = M.muon ? fmaf(M.keep, to_f32<T>(w[i][j][e]), -M.rate * x[i][j][e]) : x[i][j][e];
+        const float r = x[i][j][e] * kInvS;
+        const float v = M.muon ? fmaf(M.keep, to_f32<T>(w[i][j][e]), -M.rate * r) : r;
         if (in) ((T*)M.out[mat])[k] = from_f32<T>(v);
     });
 }
@@ -306,6 +346,12 @@ struct Half {
     int ld;
 };
 
+__device__ __forceinline__ void put_halves(float v, const Half& H, int64_t i) {
+    f16x2 hi, lo;
+    split2(v * kS, 0.f, hi, lo);
+    H.hi[i] = hi[0], H.lo[i] = lo[0];
+}
+
 // X0 in both orders, zeros in the padding.  64 x 64 tiles of X; 256 threads.
 template <class T>
 __global__ __launch_bounds__(256) void ortho_split_kernel(Mats M, const double* part, Half X, Half Xt) {
@@ -339,13 +385,14 @@ __global__ __launch_bounds__(256) void ortho_split_kernel(Mats M, const double* 
     __syncthreads();
     for (int i = wave; i < 64; i += 4) {
         const int64_t a = mat * X.step + (int64_t)(r0 + i) * X.ld + c0 + lane;
-        split(tile[i][lane], X.hi[a], X.lo[a]);
+        put_halves(tile[i][lane], X, a);
         const int64_t b = mat * Xt.step + (int64_t)(c0 + i) * Xt.ld + r0 + lane;
-        split(tile[lane][i], Xt.hi[b], Xt.lo[b]);
+        put_halves(tile[lane][i], Xt, b);
     }
 }
 
-// C = ca Z + cp U V^T for [M][K] U and [N][K] V; C in both orders, or into the results.
+// S C = ca (S Z) + cp (S U) (S V)^T for [M][K] U and [N][K] V; C in both orders, or 1 / S of it into the
+// results (cp and ca hold that factor then).
 struct Prod {
     Half U, V, Z, C, Ct;
     int tm, tn, K;       // tiles over the rows and columns of C; the sum's length, a multiple of 32
@@ -478,12 +525,7 @@ __global__ __launch_bounds__(256) void ortho_product_kernel(Prod P, Mats M) {
     __syncthreads();
     auto put = [&](const Half& H, int row, int col, const float (&v)[8]) {
         f16x8 hi, lo;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            f16 a, b;
-            split(v[e], a, b);
-            hi[e] = a, lo[e] = b;
-        }
+        split<8>(v, hi, lo);
         const int64_t c = mat * H.step + (int64_t)row * H.ld + col;
         *(f16x8*)(H.hi + c) = hi;
         *(f16x8*)(H.lo + c) = lo;
@@ -497,7 +539,7 @@ __global__ __launch_bounds__(256) void ortho_product_kernel(Prod P, Mats M) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             v[e] = t[row * PT + col + e];
-            if (P.Z.hi) v[e] = fmaf(P.ca * kInvS, (float)zh[it][e] + (float)zl[it][e], v[e]);
+            if (P.Z.hi) v[e] = fmaf(P.ca, (float)zh[it][e] + (float)zl[it][e], v[e]);
         }
         if (both) {
 #pragma unroll
@@ -608,11 +650,12 @@ int run_large(const Mats& M, const OrthoPlan& p, int count, int steps, float ca,
     const Half none{nullptr, nullptr, 0, 0};
     for (int i = 0; i < steps && r == FPDE_OK; ++i) {
         const int o = i & 1;
-        r = product(Prod{X[o], X[o], none, A, A, ts, ts, (int)p.lp, 1, 0.f, kInvSS}, false);
-        if (r == FPDE_OK) r = product(Prod{A, A, A, B, B, ts, ts, (int)p.sp, 1, cb, cc * kInvSS}, false);
+        const bool last = i + 1 == steps;
+        r = product(Prod{X[o], X[o], none, A, A, ts, ts, (int)p.lp, 1, 0.f, kInvS}, false);
+        if (r == FPDE_OK) r = product(Prod{A, A, A, B, B, ts, ts, (int)p.sp, 1, cb, cc * kInvS}, false);
         if (r == FPDE_OK)
-            r = product(Prod{B, Xt[o], X[o], X[o ^ 1], Xt[o ^ 1], ts, tl, (int)p.sp, 0, ca, kInvSS},
-                        i + 1 == steps);
+            r = last ? product(Prod{B, Xt[o], X[o], none, none, ts, tl, (int)p.sp, 0, ca * kInvS, kInvSS}, true)
+                     : product(Prod{B, Xt[o], X[o], X[o ^ 1], Xt[o ^ 1], ts, tl, (int)p.sp, 0, ca, kInvS}, false);
     }
     return r;
 }

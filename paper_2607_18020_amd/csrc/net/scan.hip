@@ -55,7 +55,7 @@ struct ScanP {
     const int32_t* lengths;
     void *y, *ddelta, *dz;                // y: du in the backward
     float* state_out;
-    float *hend, *gend, *sdt;             // [batch][chunks][NS][channels], [batch][chunks][channels]
+    float *hend, *gend, *sdt;             // [chunks][batch][NS][channels], [chunks][batch][channels]
     float *ck, *cs;                       // [batch][blocks][NS][channels], [batch][blocks][channels]
     float *pbc, *pA, *pD, *pbias;         // partial sums
     int64_t batch, jobs;                  // jobs: sequences times chunks
@@ -140,15 +140,17 @@ __device__ __forceinline__ Place place(const ScanP& P) {
     return q;
 }
 
-// The chunk that a job is: sequence b, levels t0 .. tn - 1, of which those before t1 exist.
+// The chunk that a job is: sequence b, levels t0 .. tn - 1, of which those before t1 exist.  Jobs go
+// through all sequences before the next chunk: the last chunks, which short sequences do not have, are
+// then the last of every SIMD's wavefronts and not all of some SIMDs'.
 struct Job {
     int64_t b;
     int ch, t0, tn, t1;
 };
 __device__ __forceinline__ Job job_of(const ScanP& P, int64_t i) {
     Job j;
-    j.b = P.chunks == 1 ? i : i / P.chunks;
-    j.ch = P.chunks == 1 ? 0 : (int)(i - j.b * P.chunks);
+    j.ch = P.chunks == 1 ? 0 : (int)(i / P.batch);
+    j.b = i - j.ch * P.batch;
     const int len = levels(P.lengths, j.b, P.length);
     j.t0 = j.ch * P.chunk;
     j.tn = j.t0 + P.chunk < P.length ? j.t0 + P.chunk : P.length;
@@ -156,14 +158,19 @@ __device__ __forceinline__ Job job_of(const ScanP& P, int64_t i) {
     return j;
 }
 
-// (the row's address is the wavefront's, so only the channel takes a lane's register)
+// Element i of a row.  The row's address is the wavefront's; the lane's part is an offset in bytes below
+// 2^32, which the memory instructions add by themselves.
 template <class T>
-__device__ __forceinline__ T at(const Seq& s, int64_t b, int t, int c) {
-    return ((const T*)s.p + b * s.bs + (int64_t)t * s.ts)[(unsigned)c];
+__device__ __forceinline__ T get(const T* row, int i) {
+    return *(const T*)((const char*)row + (unsigned)(i * (int)sizeof(T)));
 }
 template <class T>
-__device__ __forceinline__ void put(void* p, int64_t row, int channels, int c, float v) {
-    ((T*)p + row * channels)[(unsigned)c] = from_f32<T>(v);
+__device__ __forceinline__ void put(T* row, int i, T v) {
+    *(T*)((char*)row + (unsigned)(i * (int)sizeof(T))) = v;
+}
+template <class T>
+__device__ __forceinline__ T at(const Seq& s, int64_t b, int t, int c) {
+    return get((const T*)s.p + b * s.bs + (int64_t)t * s.ts, c);
 }
 
 // B and C of a block of K levels in LDS: row j holds B's NS numbers, then C's (zeros past the states
@@ -174,14 +181,16 @@ struct Tile {
     Raw<T, 4> q[Q];
     // starts the loads of levels t .. t + K - 1 (those from t1 on are the last one again)
     __device__ __forceinline__ void load(const ScanP& P, int64_t b, int g, int t, int t1) {
+        const T* pb = (const T*)P.B.p + b * P.B.bs + (int64_t)g * P.states;
+        const T* pc = (const T*)P.C.p + b * P.C.bs + (int64_t)g * P.states;
+        const int64_t bts = P.B.ts, cts = P.C.ts;
 #pragma unroll
         for (int i = 0; i < Q; ++i) {
             const int e = i * 64 + (int)threadIdx.x, j = e / (ROW / 4), r = e % (ROW / 4) * 4;
             const bool is_c = r >= NS;
             int n = is_c ? r - NS : r;
             const int l = t + j < t1 ? t + j : t1 - 1;
-            const T* p = (const T*)(is_c ? P.C.p : P.B.p) + b * (is_c ? P.C.bs : P.B.bs) +
-                         (int64_t)l * (is_c ? P.C.ts : P.B.ts) + (int64_t)g * P.states;
+            const T* p = is_c ? pc + l * cts : pb + l * bts;
             if (P.states % 4 == 0) {
                 q[i] = load_raw<T, 4>(p + (n < P.states ? n : 0));
             } else {
@@ -233,12 +242,12 @@ __device__ __forceinline__ void load_carried(float (&h)[NS], const ScanP& P, int
 template <int NS>
 __device__ __forceinline__ void load_states(float (&h)[NS], const float* p, const ScanP& P, int c) {
 #pragma unroll
-    for (int n = 0; n < NS; ++n, p += P.channels) h[n] = p[(unsigned)c];
+    for (int n = 0; n < NS; ++n, p += P.channels) h[n] = get(p, c);
 }
 template <int NS>
 __device__ __forceinline__ void store_states(const float (&h)[NS], float* p, const ScanP& P, int c) {
 #pragma unroll
-    for (int n = 0; n < NS; ++n, p += P.channels) p[(unsigned)c] = h[n];
+    for (int n = 0; n < NS; ++n, p += P.channels) put(p, c, h[n]);
 }
 
 // ---------------------------------------------------------------------------
@@ -257,7 +266,7 @@ struct Cursor {
     }
     // this level's value; `more`: there is another level after it
     __device__ __forceinline__ T next(int c, bool more) {
-        const T v = p[(unsigned)c];
+        const T v = get(p, c);
         p += more ? ts : 0;
         return v;
     }
@@ -393,7 +402,7 @@ __global__ __launch_bounds__(64) void scan_fwd_kernel(ScanP P) {
                 if (OUT) {
                     acc = fmaf(dd, u, acc);
                     const float z = silu(to_f32<T>(now.z[j]));
-                    out[(unsigned)c] = from_f32<T>(P.gate ? acc * z : acc);
+                    put(out, c, from_f32<T>(P.gate ? acc * z : acc));
                     out += P.channels;
                 }
                 level_fence();
@@ -401,7 +410,7 @@ __global__ __launch_bounds__(64) void scan_fwd_kernel(ScanP P) {
             now = next;
         }
         if (OUT) {
-            for (int t = J.t1 > J.t0 ? J.t1 : J.t0; t < J.tn; ++t) put<T>(P.y, row + t, P.channels, c, 0.f);
+            for (int t = J.t1 > J.t0 ? J.t1 : J.t0; t < J.tn; ++t) put((T*)P.y + (row + t) * P.channels, c, from_f32<T>(0.f));
             if (P.state_out && J.ch == P.chunks - 1) {
                 const int k = states_here(P);
                 float* s = P.state_out + (J.b * P.channels + c) * k;
@@ -436,7 +445,7 @@ __global__ __launch_bounds__(512) void chunk_kernel(ScanP P, int ns, float* e, f
             const bool idle = first >= P.chunks;  // (a wavefront without chunks only keeps the barriers)
             auto job = [&](int k) {
                 const int i = first + k < P.chunks ? first + k : P.chunks - 1;
-                return b * P.chunks + (back ? P.chunks - 1 - i : i);
+                return (back ? P.chunks - 1 - i : i) * P.batch + b;
             };
             float* s = back ? e2 : e;
             if (!idle) {
@@ -555,7 +564,7 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2))) void sc
             }
             const int64_t k = J.b * blocks + t / KB;
             store_states<NS>(h, Q.ck + k * NS * P.channels, P, c);
-            if (SPLIT) (Q.cs + k * P.channels)[(unsigned)c] = sum;
+            if (SPLIT) put(Q.cs + k * P.channels, c, sum);
             in_block<KB>(J.t1 - t, [&](int j) {
                 const Row<NS> w = row_of<NS>(bc, j);
                 const float u = to_f32<T>(now.u[j]), raw = to_f32<T>(now.d[j]) + bias;
@@ -665,12 +674,12 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2, 2))) void
             dA[n] = 0.f;
         }
     }
-    const unsigned at_n = (unsigned)(n0 * P.channels + c);  // of the lane's first state in a row of states
+    const int at_n = n0 * P.channels + c;  // of the lane's first state in a row of states
     const float bias = P.bias ? P.bias[c] : 0.f, dd = P.D ? P.D[c] : 0.f;
     float dD = 0.f, dbias = 0.f;
     auto states = [&](float (&h)[NL], const float* p) {
 #pragma unroll
-        for (int n = 0; n < NL; ++n, p += P.channels) h[n] = p[at_n];
+        for (int n = 0; n < NL; ++n, p += P.channels) h[n] = get(p, at_n);
     };
     for (int64_t i = q.row; i < P.jobs; i += P.rows) {
         const Job J = job_of(P, i);
@@ -698,7 +707,7 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2, 2))) void
             states(h, Q.ck + k * NS * P.channels);
             if (P.chunks > 1) {
                 // the state that the chunk starts from, decayed to the block
-                const float sum = (Q.cs + k * P.channels)[(unsigned)c];
+                const float sum = get(Q.cs + k * P.channels, c);
                 float hc[NL];
                 states(hc, Q.hend + i * NS * P.channels);
 #pragma unroll
@@ -728,7 +737,7 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2, 2))) void
                 const float dout = to_f32<T>(raws.g[j]), z = to_f32<T>(raws.z[j]), s = sigmoid(z);
                 dy[j] = P.gate ? dout * (z * s) : dout;
                 // (a channel's lanes store the same value)
-                if (P.gate) dz_out[(unsigned)c] = from_f32<T>(dout * y * (s * fmaf(z, 1.f - s, 1.f)));
+                if (P.gate) put(dz_out, c, from_f32<T>(dout * y * (s * fmaf(z, 1.f - s, 1.f))));
                 dz_out += P.channels;
                 level_fence();
             });
@@ -765,20 +774,20 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2, 2))) void
                 dl = P.softplus ? dl * slope : dl;
                 dD = fmaf(dy[j], u[j], dD);
                 dbias += dl;
-                du_out[(unsigned)c] = from_f32<T>(fmaf(dt, gB, dd * dy[j]));
-                dd_out[(unsigned)c] = from_f32<T>(dl);
+                put(du_out, c, from_f32<T>(fmaf(dt, gB, dd * dy[j])));
+                put(dd_out, c, from_f32<T>(dl));
                 du_out -= P.channels, dd_out -= P.channels;
                 // value n of both sums is in L lanes of the part's
                 constexpr int L = 64 / NS;
-                if (lane % L < 2) bc_out[(unsigned)(lane / L + lane % L * NS)] = lane % L ? sc : sb;
+                if (lane % L < 2) put(bc_out, lane / L + lane % L * NS, lane % L ? sc : sb);
                 bc_out -= 2 * NS;
                 level_fence();
             });
         }
         for (int t = J.t1 > J.t0 ? J.t1 : J.t0; t < J.tn; ++t) {
-            put<T>(P.y, row + t, P.channels, c, 0.f);
-            put<T>(P.ddelta, row + t, P.channels, c, 0.f);
-            if (P.gate) put<T>(P.dz, row + t, P.channels, c, 0.f);
+            put((T*)P.y + (row + t) * P.channels, c, from_f32<T>(0.f));
+            put((T*)P.ddelta + (row + t) * P.channels, c, from_f32<T>(0.f));
+            if (P.gate) put((T*)P.dz + (row + t) * P.channels, c, from_f32<T>(0.f));
         }
     }
     if (!q.live) return;
@@ -830,7 +839,7 @@ struct Plan {
 // Wavefronts that fill the card: one for each SIMD.  Whole windows with fewer are
 // split in chunks until there are kWaves, as long as a chunk keeps kMinChunk levels.
 constexpr int64_t kFill = 1024, kWaves = 4096;
-constexpr int kMinChunk = 32;
+constexpr int kMinChunk = 16;
 // Most wavefronts of a launch; of the backward's main launch, whose partial sums of dA grow with them.
 constexpr int64_t kMaxWaves = (int64_t)1 << 24, kBwdWaves = 8192;
 
