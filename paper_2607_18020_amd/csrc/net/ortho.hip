@@ -111,14 +111,21 @@ __device__ __forceinline__ float inv_norm(double sumsq, float eps) {
 // ---------------------------------------------------------------------------
 // Small matrices.
 
-// Products of rows of U and rows of V, both [rows][pitch] in LDS, hi then lo `hu`, `hv` elements
-// later: MT x NT tiles of 16 x 16.  A lane reads 8 neighbouring k of row l % 16; the next 32 k are
-// read while these are multiplied.
-template <int MT, int NT, int K>
-__device__ __forceinline__ void lds_product(f32x4 (&acc)[MT][NT], const f16* U, int pu, int hu, const f16* V,
-                                            int pv, int hv) {
+// An operand in LDS: 8 neighbouring k of a row are 16 bytes, those of the next row follow, and the next 8 k
+// come after all rows.  So 16 lanes that read 16 rows, whatever k each reads, meet every bank once.
+template <int ROWS>
+__device__ __forceinline__ int spot(int row, int k) {
+    return (k >> 3) * (ROWS * 8) + row * 8 + (k & 7);
+}
+
+// Products of MT x NT tiles of 16 x 16 rows: U's from row u0 on with V's from v0 on; lo lies `hu`, `hv`
+// elements after hi.  A lane reads 8 neighbouring k of row l % 16; the next 32 k are read while these
+// are multiplied.
+template <int MT, int NT, int K, int UR, int VR>
+__device__ __forceinline__ void lds_product(f32x4 (&acc)[MT][NT], const f16* U, int u0, int hu, const f16* V,
+                                            int v0, int hv) {
     const int lane = (int)(threadIdx.x & 63), r = lane & 15, k0 = (lane >> 4) * 8;
-    U += r * pu + k0, V += r * pv + k0;
+    U += spot<UR>(u0 + r, k0), V += spot<VR>(v0 + r, k0);
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -127,13 +134,13 @@ __device__ __forceinline__ void lds_product(f32x4 (&acc)[MT][NT], const f16* U, 
     auto read = [&](int b, int k) {
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-            vl[b][j] = *(const f16x8*)(V + hv + j * 16 * pv + k);
-            vh[b][j] = *(const f16x8*)(V + j * 16 * pv + k);
+            vl[b][j] = *(const f16x8*)(V + hv + spot<VR>(j * 16, k));
+            vh[b][j] = *(const f16x8*)(V + spot<VR>(j * 16, k));
         }
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-            uh[b][i] = *(const f16x8*)(U + i * 16 * pu + k);
-            ul[b][i] = *(const f16x8*)(U + hu + i * 16 * pu + k);
+            uh[b][i] = *(const f16x8*)(U + spot<UR>(i * 16, k));
+            ul[b][i] = *(const f16x8*)(U + hu + spot<UR>(i * 16, k));
         }
     };
     read(0, 0);
@@ -161,17 +168,17 @@ struct Quad {
         *(f16x4*)p = hi;
         *(f16x4*)(p + half) = lo;
     }
-    // The same by rows, `pitch` apart, from p on.  Neighbouring lanes hold neighbouring columns; the even one
-    // takes the first two rows of both and the odd one the others, so that a write is two columns wide.
-    __device__ __forceinline__ void put_rows(f16* p, int pitch, int half) const {
+    // The same as k of four rows, p being the first one's.  Neighbouring lanes hold neighbouring k; the even
+    // one takes the first two rows of both and the odd one the others, so that a write is two k wide.
+    __device__ __forceinline__ void put_rows(f16* p, int half) const {
         const bool odd = threadIdx.x & 1;
-        p += odd ? 2 * pitch - 1 : 0;
-        two_rows(hi, p, pitch, odd);
-        two_rows(lo, p + half, pitch, odd);
+        p += odd ? 2 * 8 - 1 : 0;
+        two_rows(hi, p, odd);
+        two_rows(lo, p + half, odd);
     }
 
 private:
-    static __device__ __forceinline__ void two_rows(const f16x4& v, f16* p, int pitch, bool odd) {
+    static __device__ __forceinline__ void two_rows(const f16x4& v, f16* p, bool odd) {
         struct Words {
             uint32_t a, b;
         };
@@ -181,16 +188,15 @@ private:
         const uint32_t even_col = odd ? other : mine, odd_col = odd ? mine : other;
         // (byte selections: the low halves of both, the high halves of both)
         *(uint32_t*)p = __builtin_amdgcn_perm(odd_col, even_col, 0x05040100);
-        *(uint32_t*)(p + pitch) = __builtin_amdgcn_perm(odd_col, even_col, 0x07060302);
+        *(uint32_t*)(p + 8) = __builtin_amdgcn_perm(odd_col, even_col, 0x07060302);
     }
 };
 
 // One workgroup of 8 wavefronts, 2 x 4 of them over the rows and columns of X, a matrix.
 template <class T, int SP, int LP>
 __global__ __launch_bounds__(512) void ortho_small_kernel(Mats M, int steps, float ca, float cb, float cc) {
-    constexpr int PS = SP + 8, PL = LP + 8;                // pitches: rows 16 bytes apart in the banks
-    constexpr int HR = SP * PL, HT = LP * PS, HA = SP * PS;  // elements of X, X^T, A or B
-    constexpr int R1 = HR > HA ? HR : HA, R2 = HT > HA ? HT : HA;
+    // elements of X by rows and, after it, B; of A and, after it, X by columns
+    constexpr int R1 = SP * LP > SP * SP ? SP * LP : SP * SP, R2 = R1;
     static_assert((R1 + R2) * 4 + 64 <= 160 * 1024, "LDS");
     __shared__ __attribute__((aligned(16))) f16 lds1[2 * R1];
     __shared__ __attribute__((aligned(16))) f16 lds2[2 * R2];
@@ -255,10 +261,10 @@ __global__ __launch_bounds__(512) void ortho_small_kernel(Mats M, int steps, flo
         for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int j = 0; j < NT; ++j)
-                Quad(x[i][j]).put_rows(lds1 + (row0 + i * 16 + r4) * PL + col0 + j * 16 + cl, PL, R1);
+                Quad(x[i][j]).put_rows(lds1 + spot<SP>(row0 + i * 16 + r4, col0 + j * 16 + cl), R1);
         __syncthreads();
         f32x4 acc[MT][AT];
-        lds_product<MT, AT, LP>(acc, lds1 + row0 * PL, PL, R1, lds1 + acol0 * PL, PL, R1);
+        lds_product<MT, AT, LP, SP, SP>(acc, lds1, row0, R1, lds1, acol0, R1);
         float A[MT][AT][4];
 #pragma unroll
         for (int i = 0; i < MT; ++i)
@@ -266,10 +272,10 @@ __global__ __launch_bounds__(512) void ortho_small_kernel(Mats M, int steps, flo
             for (int j = 0; j < AT; ++j) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) A[i][j][e] = acc[i][j][e] * kInvS;
-                Quad(A[i][j]).put(lds2 + (acol0 + j * 16 + cl) * PS + row0 + i * 16 + r4, R2);  // (symmetric)
+                Quad(A[i][j]).put(lds2 + spot<SP>(acol0 + j * 16 + cl, row0 + i * 16 + r4), R2);  // (symmetric)
             }
         __syncthreads();
-        lds_product<MT, AT, SP>(acc, lds2 + row0 * PS, PS, R2, lds2 + acol0 * PS, PS, R2);
+        lds_product<MT, AT, SP, SP, SP>(acc, lds2, row0, R2, lds2, acol0, R2);
         // (every wavefront is past its reads of X by rows: B takes its place)
 #pragma unroll
         for (int i = 0; i < MT; ++i)
@@ -278,17 +284,17 @@ __global__ __launch_bounds__(512) void ortho_small_kernel(Mats M, int steps, flo
                 float b[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) b[e] = fmaf(cb, A[i][j][e], cc * kInvS * acc[i][j][e]);
-                Quad(b).put(lds1 + (acol0 + j * 16 + cl) * PS + row0 + i * 16 + r4, R1);
+                Quad(b).put(lds1 + spot<SP>(acol0 + j * 16 + cl, row0 + i * 16 + r4), R1);
             }
         __syncthreads();  // (and past those of A: X by columns takes its place)
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int j = 0; j < NT; ++j)
-                Quad(x[i][j]).put(lds2 + (col0 + j * 16 + cl) * PS + row0 + i * 16 + r4, R2);
+                Quad(x[i][j]).put(lds2 + spot<LP>(col0 + j * 16 + cl, row0 + i * 16 + r4), R2);
         __syncthreads();
         f32x4 y[MT][NT];
-        lds_product<MT, NT, SP>(y, lds1 + row0 * PS, PS, R1, lds2 + col0 * PS, PS, R2);
+        lds_product<MT, NT, SP, SP, LP>(y, lds1, row0, R1, lds2, col0, R2);
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
