@@ -223,20 +223,20 @@ __device__ __forceinline__ int states_here(const ScanP& P) {
     asm volatile("" : "+s"(n));
     return n;
 }
-// A * log2(e) of one channel (0 past the states that exist)
+// A * log2(e) of one channel's states from n0 on (0 past those that exist)
 template <int NS>
-__device__ __forceinline__ void load_a2(const ScanP& P, int c, float (&a2)[NS]) {
+__device__ __forceinline__ void load_a2(const ScanP& P, int c, int n0, float (&a2)[NS]) {
     const int k = states_here(P);
 #pragma unroll
-    for (int n = 0; n < NS; ++n) a2[n] = n < k ? P.A[(int64_t)c * k + n] * kLog2e : 0.f;
+    for (int n = 0; n < NS; ++n) a2[n] = n0 + n < k ? P.A[(int64_t)c * k + n0 + n] * kLog2e : 0.f;
 }
 // the carried state of one channel, or zeros
 template <int NS>
-__device__ __forceinline__ void load_carried(float (&h)[NS], const ScanP& P, int64_t b, int c) {
+__device__ __forceinline__ void load_carried(float (&h)[NS], const ScanP& P, int64_t b, int c, int n0) {
     const int k = states_here(P);
     const float* s = P.state ? P.state + (b * P.channels + c) * k : nullptr;
 #pragma unroll
-    for (int n = 0; n < NS; ++n) h[n] = s && n < k ? s[n] : 0.f;
+    for (int n = 0; n < NS; ++n) h[n] = s && n0 + n < k ? s[n0 + n] : 0.f;
 }
 // a row of states, [NS][channels] from p on (those past the states that exist are 0 throughout)
 template <int NS>
@@ -349,15 +349,16 @@ __device__ __forceinline__ void back_guarded(int n, F f) {
 }
 
 template <class T, int NS, bool OUT>
-__global__ __launch_bounds__(64) void scan_fwd_kernel(ScanP P) {
+__global__ __launch_bounds__(64) void scan_fwd_kernel(ScanP args) {
     constexpr int K = 8;
     __shared__ __attribute__((aligned(16))) float bc[K * 2 * NS];
-    const Place q = place(P);
+    const Place q = place(args);
     const int c = q.c;
     float a2[NS];
-    load_a2<NS>(P, c, a2);
-    const float bias = P.bias ? P.bias[c] : 0.f, dd = OUT && P.D ? P.D[c] : 0.f;
-    for (int64_t i = q.row; i < P.jobs; i += P.rows) {
+    load_a2<NS>(args, c, 0, a2);
+    const float bias = args.bias ? args.bias[c] : 0.f, dd = OUT && args.D ? args.D[c] : 0.f;
+    for (int64_t i = q.row; i < args.jobs; i += args.rows) {
+        const ScanP P = args_again();
         const Job J = job_of(P, i);
         Block<T, K> now, next;
         Cursors<T> in;
@@ -372,7 +373,7 @@ __global__ __launch_bounds__(64) void scan_fwd_kernel(ScanP P) {
         if (OUT && P.chunks > 1) {
             load_states<NS>(h, P.hend + i * NS * P.channels, P, c);
         } else if (OUT) {
-            load_carried<NS>(h, P, J.b, c);
+            load_carried<NS>(h, P, J.b, c, 0);
         } else {
 #pragma unroll
             for (int n = 0; n < NS; ++n) h[n] = 0.f;
@@ -530,17 +531,18 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanP P) {
 // Forward through the window: the state at the start of every block of KB levels.  SPLIT: from zero
 // at the chunk's start, with the sum of dt before the block; and what the chunk adds to the state after it and
 // to the adjoint state before it.
-template <class T, int NS, int KB, bool SPLIT>
-__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2))) void scan_pre_kernel(ScanP P) {
+template <class T, int NL, int LP, int KB, bool SPLIT>
+__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2))) void scan_pre_kernel(ScanP args) {
+    constexpr int NS = NL * LP;
     __shared__ __attribute__((aligned(16))) float bc[KB * 2 * NS];
-    constexpr bool AHEAD = !SPLIT || NS < 32;  // (4 x 32 numbers of state leave no room for a block ahead)
-    const Place q = place(P);
-    const int c = q.c;
-    const int64_t blocks = (P.length + KB - 1) / KB;
-    float a2[NS];
-    load_a2<NS>(P, c, a2);
-    const float bias = P.bias ? P.bias[c] : 0.f;
-    for (int64_t i = q.row; i < P.jobs; i += P.rows) {
+    const Place q = place<LP>(args);
+    const int c = q.c, n0 = q.part * NL, at_n = n0 * args.channels + c;
+    const int64_t blocks = (args.length + KB - 1) / KB;
+    float a2[NL];
+    load_a2<NL>(args, c, n0, a2);
+    const float bias = args.bias ? args.bias[c] : 0.f;
+    for (int64_t i = q.row; i < args.jobs; i += args.rows) {
+        const ScanP P = args_again();
         const Job J = job_of(P, i);
         Block<T, KB> now, next;
         Cursors<T> in;
@@ -550,23 +552,23 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2))) void sc
             tile.load(P, J.b, q.g, J.t0, J.t1);
             in.load(now, J.t0, J.t1, c);
         }
-        float h[NS], G[NS], prod[NS], sum = 0.f;
-        if (!SPLIT) load_carried<NS>(h, P, J.b, c);
+        float h[NL], G[NL], prod[NL], sum = 0.f;
+        if (!SPLIT) load_carried<NL>(h, P, J.b, c, n0);
 #pragma unroll
-        for (int n = 0; n < NS; ++n) h[n] = SPLIT ? 0.f : h[n], G[n] = 0.f, prod[n] = 1.f;
+        for (int n = 0; n < NL; ++n) h[n] = SPLIT ? 0.f : h[n], G[n] = 0.f, prod[n] = 1.f;
 #pragma unroll 1
         for (int t = J.t0; t < J.t1; t += KB) {
             const ScanP Q = args_again();
             tile.store(Q, bc);
             if (t + KB < J.t1) {
                 tile.load(Q, J.b, q.g, t + KB, J.t1);
-                if (AHEAD) in.load(next, t + KB, J.t1, c);
+                in.load(next, t + KB, J.t1, c);
             }
             const int64_t k = J.b * blocks + t / KB;
-            store_states<NS>(h, Q.ck + k * NS * P.channels, P, c);
+            store_states<NL>(h, Q.ck + k * NS * P.channels, P, at_n);
             if (SPLIT) put(Q.cs + k * P.channels, c, sum);
             in_block<KB>(J.t1 - t, [&](int j) {
-                const Row<NS> w = row_of<NS>(bc, j);
+                const Row<NS> w = row_of<NS>(bc, j, n0);
                 const float u = to_f32<T>(now.u[j]), raw = to_f32<T>(now.d[j]) + bias;
                 const float dt = step_of(P, raw), du = dt * u;
                 float dy = 0.f;
@@ -577,7 +579,7 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2))) void sc
                     sum += dt;
                 }
 #pragma unroll
-                for (int n = 0; n < NS; ++n) {
+                for (int n = 0; n < NL; ++n) {
                     const float a = __builtin_amdgcn_exp2f(dt * a2[n]);
                     h[n] = fmaf(a, h[n], du * w[n]);
                     if (SPLIT) {
@@ -587,14 +589,11 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2))) void sc
                 }
                 level_fence();
             });
-            if (AHEAD)
-                now = next;
-            else if (t + KB < J.t1)
-                in.load(now, t + KB, J.t1, c);
+            now = next;
         }
         if (SPLIT) {
-            store_states<NS>(h, P.hend + i * NS * P.channels, P, c);
-            store_states<NS>(G, P.gend + i * NS * P.channels, P, c);
+            store_states<NL>(h, P.hend + i * NS * P.channels, P, at_n);
+            store_states<NL>(G, P.gend + i * NS * P.channels, P, at_n);
             P.sdt[i * P.channels + c] = sum;
         }
     }
@@ -659,29 +658,25 @@ __device__ __forceinline__ float parts_sum(float v) {
 }
 
 template <class T, int NL, int LP, int KB>
-__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2, 2))) void scan_bwd_kernel(ScanP P) {
+__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2, 2))) void scan_bwd_kernel(ScanP args) {
     constexpr int NS = NL * LP;
     __shared__ __attribute__((aligned(16))) float bc[KB * 2 * NS];
-    const Place q = place<LP>(P);
+    const Place q = place<LP>(args);
     const int c = q.c, lane = (int)threadIdx.x, n0 = q.part * NL;
-    const int64_t blocks = (P.length + KB - 1) / KB;
+    const int64_t blocks = (args.length + KB - 1) / KB;
     float a2[NL], dA[NL];
-    {
-        const int k = states_here(P);
+    load_a2<NL>(args, c, n0, a2);
 #pragma unroll
-        for (int n = 0; n < NL; ++n) {
-            a2[n] = n0 + n < k ? P.A[(int64_t)c * k + n0 + n] * kLog2e : 0.f;
-            dA[n] = 0.f;
-        }
-    }
-    const int at_n = n0 * P.channels + c;  // of the lane's first state in a row of states
-    const float bias = P.bias ? P.bias[c] : 0.f, dd = P.D ? P.D[c] : 0.f;
+    for (int n = 0; n < NL; ++n) dA[n] = 0.f;
+    const int at_n = n0 * args.channels + c;  // of the lane's first state in a row of states
+    const float bias = args.bias ? args.bias[c] : 0.f, dd = args.D ? args.D[c] : 0.f;
     float dD = 0.f, dbias = 0.f;
     auto states = [&](float (&h)[NL], const float* p) {
 #pragma unroll
-        for (int n = 0; n < NL; ++n, p += P.channels) h[n] = get(p, at_n);
+        for (int n = 0; n < NL; ++n, p += args.channels) h[n] = get(p, at_n);
     };
-    for (int64_t i = q.row; i < P.jobs; i += P.rows) {
+    for (int64_t i = q.row; i < args.jobs; i += args.rows) {
+        const ScanP P = args_again();
         const Job J = job_of(P, i);
         float G[NL];  // a_{t+1} g_{t+1}
         if (P.chunks > 1) {
@@ -791,6 +786,7 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2, 2))) void
         }
     }
     if (!q.live) return;
+    const ScanP P = args_again();
     const int k = states_here(P);
     float* s = P.pA + ((int64_t)q.row * P.channels + c) * k + n0;
 #pragma unroll
@@ -828,12 +824,14 @@ constexpr int64_t kMaxChannels = 1 << 20, kMaxLevels = (int64_t)1 << 40;
 int states_of(int states) { return states <= 4 ? 4 : states <= 8 ? 8 : states <= 16 ? 16 : 32; }
 constexpr int kBlock = 8;  // levels between saved states in the backward
 // lanes of a channel in the backward's main pass
-int parts_of(int ns) { return ns <= 8 ? 1 : ns / 8; }
+constexpr int parts_of(int ns) { return ns <= 8 ? 1 : ns / 8; }
+// and in the pass before it, which holds four numbers a state, not fifteen
+constexpr int pre_parts_of(int ns) { return ns <= 16 ? 1 : ns / 16; }
 
 struct Plan {
     int nblk, per, ns, chunk, chunks;
     int64_t jobs;
-    int rows, bwd_rows, bwd_nblk;
+    int rows, pre_rows, pre_nblk, bwd_rows, bwd_nblk;
 };
 
 // Wavefronts that fill the card: one for each SIMD.  Whole windows with fewer are
@@ -860,6 +858,8 @@ Plan plan(int64_t batch, int64_t length, int64_t channels, int states, int group
         return (int)(p.jobs < 1 ? 1 : (r < 1 ? 1 : (p.jobs < r ? p.jobs : r)));
     };
     p.bwd_nblk = (int)cdiv(p.per, 64 / parts_of(p.ns));
+    p.pre_nblk = (int)cdiv(p.per, 64 / pre_parts_of(p.ns));
+    p.pre_rows = rows(kMaxWaves, p.pre_nblk);
     p.rows = rows(kMaxWaves, p.nblk), p.bwd_rows = rows(kBwdWaves, p.bwd_nblk);
     return p;
 }
@@ -1068,13 +1068,14 @@ extern "C" int fpde_selective_scan_bwd(const fpde_scan_bwd_args* a, void* stream
     if (n > 0) {
         st = with_scan(a->dtype, p, [&](auto t, auto nsc) {
             using T = decltype(t);
-            constexpr int NS = decltype(nsc)::value, KB = kBlock, LP = NS <= 8 ? 1 : NS / 8;
+            constexpr int NS = decltype(nsc)::value, KB = kBlock, LP = parts_of(NS), LQ = pre_parts_of(NS);
             int r;
+            P.rows = p.pre_rows, P.nblk = p.pre_nblk;
             if (P.chunks > 1) {
-                r = launch(scan_pre_kernel<T, NS, KB, true>, grid_of(P), dim3(64), s, P);
+                r = launch(scan_pre_kernel<T, NS / LQ, LQ, KB, true>, grid_of(P), dim3(64), s, P);
                 if (r == FPDE_OK) r = queue_chunks(P, NS, P.hend, P.gend, s);
             } else {
-                r = launch(scan_pre_kernel<T, NS, KB, false>, grid_of(P), dim3(64), s, P);
+                r = launch(scan_pre_kernel<T, NS / LQ, LQ, KB, false>, grid_of(P), dim3(64), s, P);
             }
             P.rows = p.bwd_rows, P.nblk = p.bwd_nblk;
             if (r == FPDE_OK) r = launch(scan_bwd_kernel<T, NS / LP, LP, KB>, grid_of(P), dim3(64), s, P);
