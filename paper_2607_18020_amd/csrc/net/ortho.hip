@@ -401,16 +401,33 @@ __global__ __launch_bounds__(256) void ortho_split_kernel(Mats M, const double* 
 // results (cp and ca hold that factor then).
 struct Prod {
     Half U, V, Z, C, Ct;
-    int tm, tn, K;       // tiles over the rows and columns of C; the sum's length, a multiple of 32
+    int tm, tn, tiles, K;  // tiles over the rows and columns of C, and of a matrix; the sum's length, 32 n
     int sym;             // C is square and symmetric: tiles on and above the diagonal, Ct = C
     float ca, cp;
 };
 
-// tile i of the upper triangle of t x t tiles, by rows
-__device__ __forceinline__ void triangle(int i, int t, int* r, int* c) {
-    int row = 0;
-    while (i >= t - row) i -= t - row, ++row;
-    *r = row, *c = row + i;
+// The order of the tiles: bands of 8 rows of tiles, each by columns, so that the tiles that run together
+// share rows of both operands; of a symmetric product those on and above the diagonal.
+__device__ __forceinline__ void tile_at(int i, int tm, int tn, bool sym, int* r, int* c) {
+    int r0 = 0, h = tm < 8 ? tm : 8;
+    while (true) {
+        const int corner = h * (h + 1) / 2, n = sym ? corner + h * (tn - r0 - h) : h * tn;
+        if (i < n) {
+            if (!sym) {
+                *r = r0 + i % h, *c = i / h;
+            } else if (i >= corner) {
+                i -= corner;
+                *r = r0 + i % h, *c = r0 + h + i / h;
+            } else {
+                int col = 0;
+                while (i > col) i -= ++col;
+                *r = r0 + i, *c = r0 + col;
+            }
+            return;
+        }
+        i -= n, r0 += h;
+        h = tm - r0 < 8 ? tm - r0 : 8;
+    }
 }
 
 typedef const __attribute__((address_space(1))) void* gptr_t;
@@ -427,13 +444,15 @@ __global__ __launch_bounds__(256) void ortho_product_kernel(Prod P, Mats M) {
     constexpr int OUT = TILE * PT * 4;
     constexpr int BYTES = NB * STAGE * 16 > OUT ? NB * STAGE * 16 : OUT;
     __shared__ __attribute__((aligned(16))) char lds[BYTES];
-    const int mat = (int)blockIdx.y, lane = (int)(threadIdx.x & 63);
+    const int lane = (int)(threadIdx.x & 63);
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    // Workgroups go round the 8 XCDs in turn: each XCD takes a run of neighbouring tiles, which its L2 then
+    // holds once, and not every eighth of all matrices.
+    const int all = (int)gridDim.x, whole = all & ~7, id = (int)blockIdx.x;
+    const int at = id < whole ? (id & 7) * (whole >> 3) + (id >> 3) : id;
+    const int mat = at / P.tiles;
     int tr, tc;
-    if (P.sym)
-        triangle((int)blockIdx.x, P.tm, &tr, &tc);
-    else
-        tr = (int)blockIdx.x % P.tm, tc = (int)blockIdx.x / P.tm;
+    tile_at(at - mat * P.tiles, P.tm, P.tn, P.sym, &tr, &tc);
     const f16* src[4] = {P.U.hi + mat * P.U.step + (int64_t)tr * TILE * P.U.ld,
                          P.U.lo + mat * P.U.step + (int64_t)tr * TILE * P.U.ld,
                          P.V.hi + mat * P.V.step + (int64_t)tc * TILE * P.V.ld,
@@ -644,9 +663,9 @@ int run_large(const Mats& M, const OrthoPlan& p, int count, int steps, float ca,
     if (r == FPDE_OK)
         r = launch(ortho_split_kernel<T>, dim3((unsigned)(p.lp / 64), (unsigned)(p.sp / 64), count), dim3(256), s,
                    M, part, X[0], Xt[0]);
-    const int ts = (int)(p.sp / p.tile), tl = (int)(p.lp / p.tile);
+    const int ts = (int)(p.sp / p.tile), tl = (int)(p.lp / p.tile), tri = ts * (ts + 1) / 2;
     auto product = [&](const Prod& P, bool last) {
-        const dim3 g((unsigned)(P.sym ? ts * (ts + 1) / 2 : P.tm * P.tn), count), b(256);
+        const dim3 g((unsigned)(P.tiles * count)), b(256);
         if (p.tile == 128)
             return last ? launch(ortho_product_kernel<128, true, T>, g, b, s, P, M)
                         : launch(ortho_product_kernel<128, false, float>, g, b, s, P, M);
@@ -657,11 +676,11 @@ int run_large(const Mats& M, const OrthoPlan& p, int count, int steps, float ca,
     for (int i = 0; i < steps && r == FPDE_OK; ++i) {
         const int o = i & 1;
         const bool last = i + 1 == steps;
-        r = product(Prod{X[o], X[o], none, A, A, ts, ts, (int)p.lp, 1, 0.f, kInvS}, false);
-        if (r == FPDE_OK) r = product(Prod{A, A, A, B, B, ts, ts, (int)p.sp, 1, cb, cc * kInvS}, false);
+        r = product(Prod{X[o], X[o], none, A, A, ts, ts, tri, (int)p.lp, 1, 0.f, kInvS}, false);
+        if (r == FPDE_OK) r = product(Prod{A, A, A, B, B, ts, ts, tri, (int)p.sp, 1, cb, cc * kInvS}, false);
         if (r == FPDE_OK)
-            r = last ? product(Prod{B, Xt[o], X[o], none, none, ts, tl, (int)p.sp, 0, ca * kInvS, kInvSS}, true)
-                     : product(Prod{B, Xt[o], X[o], X[o ^ 1], Xt[o ^ 1], ts, tl, (int)p.sp, 0, ca, kInvS}, false);
+            r = last ? product(Prod{B, Xt[o], X[o], none, none, ts, tl, ts * tl, (int)p.sp, 0, ca * kInvS, kInvSS}, true)
+                     : product(Prod{B, Xt[o], X[o], X[o ^ 1], Xt[o ^ 1], ts, tl, ts * tl, (int)p.sp, 0, ca, kInvS}, false);
     }
     return r;
 }

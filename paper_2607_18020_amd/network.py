@@ -30,7 +30,7 @@ from typing import Optional
 import torch
 
 from . import binding
-from .binding import FPDE_OK, FpdeError, _stream, _used_on
+from .binding import FPDE_OK, FpdeError, _raw_stream, _stream, _used_on
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libfpde_net.so")
@@ -134,7 +134,7 @@ def _fn(name):
 
 
 def _call(name, args, stream):
-    st = _fn(name)(args, _stream(stream))
+    st = _fn(name)(args, _raw_stream(_device_now()) if stream is None and _raw_stream else _stream(stream))
     if st != FPDE_OK:
         raise FpdeError(st, name)
 
@@ -159,49 +159,49 @@ def _workspace(name, args, dev, stream):
 # few attribute reads.)
 
 _Tensor, _F32 = torch.Tensor, torch.float32
-_device_now = torch.cuda.current_device
+_device_now = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)  # (a CUDA tensor is there)
 
 
-def _data(what, t, dev=None, dtype=None):
-    """A data tensor's type code; on the current device, or on ``dev``."""
+def _data(what, name, t):
+    """A data tensor's type code; it has to be on the current device."""
     if not isinstance(t, _Tensor) or not t.is_cuda:
-        raise ValueError(f"{what}: need a CUDA tensor")
-    dt = t.dtype
-    code = _CODES.get(dt)
-    if code is None or (dtype is not None and dt is not dtype):
-        raise ValueError(f"{what}: dtype {dt}, need " +
-                         (str(dtype) if dtype is not None else "float32, bfloat16 or float16"))
-    if dev is None:
-        if t.get_device() != _device_now():
-            raise ValueError(f"{what}: tensor on {t.device}, current device is cuda:{_device_now()}")
-    elif t.device != dev:
-        raise ValueError(f"{what}: tensors on different devices ({dev}, {t.device})")
+        raise ValueError(f"{what} {name}: need a CUDA tensor")
+    code = _CODES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{what} {name}: dtype {t.dtype}, need float32, bfloat16 or float16")
+    if t.get_device() != _device_now():
+        raise ValueError(f"{what} {name}: tensor on {t.device}, current device is cuda:{_device_now()}")
     return code
 
 
-def _dense(what, t, shape, dtype, dev):
-    """A dense tensor of this shape, type and device."""
-    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.shape != shape or t.device != dev \
-            or not t.is_contiguous():
-        raise ValueError(f"{what}: need a contiguous {dtype} tensor of shape {tuple(shape)} on {dev}")
+def _like(what, name, t, x):
+    """A tensor of x's shape, type and device; its strides are its own."""
+    if not isinstance(t, _Tensor) or t.shape != x.shape or t.dtype is not x.dtype or t.device != x.device:
+        raise ValueError(f"{what} {name}: need a tensor like the first, {tuple(x.shape)} {x.dtype} on {x.device}")
     return t.data_ptr()
 
 
-def _param(what, t, shape, dtype, dev):
+def _dense(what, name, t, shape, dtype, dev):
+    """A dense tensor of this shape, type and device."""
+    if not isinstance(t, _Tensor) or t.dtype is not dtype or t.shape != shape or t.device != dev \
+            or not t.is_contiguous():
+        raise ValueError(f"{what} {name}: need a contiguous {dtype} tensor of shape {tuple(shape)} on {dev}")
+    return t.data_ptr()
+
+
+def _param(what, name, t, shape, dtype, dev):
     """A dense parameter in float32 or the data's type."""
-    if not isinstance(t, torch.Tensor) or t.dtype not in (torch.float32, dtype):
-        raise ValueError(f"{what}: need a float32 or {dtype} tensor")
-    return _dense(what, t, shape, t.dtype, dev)
+    return _dense(what, name, t, shape, dtype if isinstance(t, _Tensor) and t.dtype is dtype else _F32, dev)
 
 
-def _rows(what, t):
+def _rows(what, name, t):
     """(rows, width, row stride) of a tensor whose leading axes fold into one."""
     n = t.dim()
     if n and t.is_contiguous():
         width = t.shape[-1]
         return (t.numel() // width if width else 0), width, width
     if n == 0 or (t.shape[-1] > 1 and t.stride(-1) != 1):
-        raise ValueError(f"{what}: the last axis has to be dense")
+        raise ValueError(f"{what} {name}: the last axis has to be dense")
     width = t.shape[-1]
     rows, stride = 1, width
     for a in range(n - 2, -1, -1):
@@ -210,17 +210,17 @@ def _rows(what, t):
         if rows == 1:
             stride = t.stride(a)
         elif t.stride(a) != stride * rows:
-            raise ValueError(f"{what}: leading axes with strides {t.stride()} do not fold into rows")
+            raise ValueError(f"{what} {name}: leading axes with strides {t.stride()} do not fold into rows")
         rows *= t.shape[a]
     if rows > 1 and stride < width:
-        raise ValueError(f"{what}: rows with strides {t.stride()} overlap")
+        raise ValueError(f"{what} {name}: rows with strides {t.stride()} overlap")
     return rows, width, max(stride, width)
 
 
-def _levels(what, t):
+def _levels(what, name, t):
     """(batch, length, channels, batch stride, time stride) of a [B, L, D] tensor."""
     if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
-        raise ValueError(f"{what}: need [batch, length, channels] with dense channels")
+        raise ValueError(f"{what} {name}: need [batch, length, channels] with dense channels")
     return (*t.shape, t.stride(0), t.stride(1))
 
 
@@ -231,11 +231,11 @@ def _empty(stream, shape, dtype, dev):
     return t
 
 
-def _empty_like(stream, x):
+def _empty_like(stream, x, dtype=None):
     """A dense tensor like x."""
     if not x.is_contiguous():
-        return _empty(stream, x.shape, x.dtype, x.device)
-    t = torch.empty_like(x)
+        return _empty(stream, x.shape, dtype or x.dtype, x.device)
+    t = torch.empty_like(x) if dtype is None else torch.empty_like(x, dtype=dtype)
     if stream is not None:
         _used_on(stream, t)
     return t
@@ -253,32 +253,30 @@ def fpde_rms_norm(x, weight=None, *, residual=None, eps: float = 1e-6, quant: Op
     float32 scale per group; returns (q, scales, s), y being about q * scale.
     ``out`` / ``sum_out``: dense tensors to write y (or q) and s to; ``sum_out`` may be
     a dense x or residual.  Leading axes of any strides that fold into rows."""
-    code = _data("fpde_rms_norm x", x)
+    code = _data("fpde_rms_norm", "x", x)
     dev, dt = x.device, x.dtype
-    rows, width, xs = _rows("fpde_rms_norm x", x)
+    rows, width, xs = _rows("fpde_rms_norm", "x", x)
     rp = rs = sp = None
     if residual is not None:
-        _data("fpde_rms_norm residual", residual, dev, dt)
-        if residual.shape != x.shape:
-            raise ValueError(f"fpde_rms_norm: residual {tuple(residual.shape)} is not like x {tuple(x.shape)}")
-        rs, rp = _rows("fpde_rms_norm residual", residual)[2], residual.data_ptr()
+        rp = _like("fpde_rms_norm", "residual", residual, x)
+        rs = _rows("fpde_rms_norm", "residual", residual)[2]
     if sum_out is not None:
-        sp = _dense("fpde_rms_norm sum_out", sum_out, x.shape, dt, dev)
+        sp = _dense("fpde_rms_norm", "sum_out", sum_out, x.shape, dt, dev)
     elif residual is not None:
         sum_out = _empty_like(stream, x)
         sp = sum_out.data_ptr()
     wp, wcode = None, code
     if weight is not None:
-        wp, wcode = _param("fpde_rms_norm weight", weight, (width,), dt, dev), _CODES[weight.dtype]
+        wp, wcode = _param("fpde_rms_norm", "weight", weight, (width,), dt, dev), _CODES[weight.dtype]
     scales = None
     odt = dt if quant is None else torch.float8_e4m3fn
     if out is None:
-        out = _empty_like(stream, x) if quant is None else _empty(stream, x.shape, odt, dev)
+        out = _empty_like(stream, x, odt)
     else:
-        _dense("fpde_rms_norm out", out, x.shape, odt, dev)
+        _dense("fpde_rms_norm", "out", out, x.shape, odt, dev)
     if quant is not None:
         groups = 1 if quant == 0 else -(-width // quant)
-        scales = _empty(stream, (*x.shape[:-1], groups), torch.float32, dev)
+        scales = _empty(stream, (rows, groups) if x.dim() == 2 else (*x.shape[:-1], groups), _F32, dev)
     a = NormArgs(code, wcode, code if quant is None else _F8, quant or 0, rows, width, xs, rs or 0, eps,
                  x.data_ptr(), rp, wp, out.data_ptr(), sp, None if scales is None else scales.data_ptr())
     _call("fpde_rms_norm", a, stream)
@@ -292,28 +290,24 @@ def fpde_rms_norm_bwd(dy, s, weight=None, *, dsum=None, eps: float = 1e-6, want_
     the forward returned, ``dsum`` the gradient that reaches it by the residual
     stream; ds is the gradient of x and of the residual alike.  ``ds`` may be a
     dense dy or dsum, updated in place.  dweight is None without a weight."""
-    code = _data("fpde_rms_norm_bwd dy", dy)
+    code = _data("fpde_rms_norm_bwd", "dy", dy)
     dev, dt = dy.device, dy.dtype
-    _data("fpde_rms_norm_bwd s", s, dev, dt)
-    if s.shape != dy.shape:
-        raise ValueError(f"fpde_rms_norm_bwd: s {tuple(s.shape)} is not like dy {tuple(dy.shape)}")
-    rows, width, dys = _rows("fpde_rms_norm_bwd dy", dy)
-    ss = _rows("fpde_rms_norm_bwd s", s)[2]
+    _like("fpde_rms_norm_bwd", "s", s, dy)
+    rows, width, dys = _rows("fpde_rms_norm_bwd", "dy", dy)
+    ss = _rows("fpde_rms_norm_bwd", "s", s)[2]
     dp, dss = None, 0
     if dsum is not None:
-        _data("fpde_rms_norm_bwd dsum", dsum, dev, dt)
-        if dsum.shape != dy.shape:
-            raise ValueError(f"fpde_rms_norm_bwd: dsum {tuple(dsum.shape)} is not like dy {tuple(dy.shape)}")
-        dss, dp = _rows("fpde_rms_norm_bwd dsum", dsum)[2], dsum.data_ptr()
+        dp = _like("fpde_rms_norm_bwd", "dsum", dsum, dy)
+        dss = _rows("fpde_rms_norm_bwd", "dsum", dsum)[2]
     wp, wcode, dweight = None, code, None
     if weight is not None:
-        wp, wcode = _param("fpde_rms_norm_bwd weight", weight, (width,), dt, dev), _CODES[weight.dtype]
+        wp, wcode = _param("fpde_rms_norm_bwd", "weight", weight, (width,), dt, dev), _CODES[weight.dtype]
         if want_dweight:
             dweight = _empty(stream, (width,), weight.dtype, dev)
     if ds is None:
         ds = _empty_like(stream, dy)
     else:
-        _dense("fpde_rms_norm_bwd ds", ds, dy.shape, dt, dev)
+        _dense("fpde_rms_norm_bwd", "ds", ds, dy.shape, dt, dev)
     a = NormBwdArgs(code, wcode, rows, width, dys, ss, dss, eps, dy.data_ptr(), s.data_ptr(), dp, wp,
                     ds.data_ptr(), None if dweight is None else dweight.data_ptr(), None, 0)
     _workspace("fpde_rms_norm_bwd", a, dev, stream)
@@ -345,16 +339,16 @@ class RmsNorm(torch.autograd.Function):
 # Short causal convolution along time.
 
 def _conv_common(what, x, weight, bias, state, lengths):
-    code = _data(f"{what} x", x)
+    code = _data(what, "x", x)
     dev, dt = x.device, x.dtype
-    B, L, D, bs, ts = _levels(f"{what} x", x)
+    B, L, D, bs, ts = _levels(what, "x", x)
     if not isinstance(weight, torch.Tensor) or weight.dim() != 2:
         raise ValueError(f"{what} weight: need [channels, taps]")
     W = weight.shape[1]
-    wp = _param(f"{what} weight", weight, (D, W), dt, dev)
-    bp = None if bias is None else _dense(f"{what} bias", bias, (D,), weight.dtype, dev)
-    sp = None if state is None else _dense(f"{what} state", state, (B, W - 1, D), dt, dev)
-    lp = None if lengths is None else _dense(f"{what} lengths", lengths, (B,), torch.int32, dev)
+    wp = _param(what, "weight", weight, (D, W), dt, dev)
+    bp = None if bias is None else _dense(what, "bias", bias, (D,), weight.dtype, dev)
+    sp = None if state is None else _dense(what, "state", state, (B, W - 1, D), dt, dev)
+    lp = None if lengths is None else _dense(what, "lengths", lengths, (B,), torch.int32, dev)
     return code, B, L, D, bs, ts, W, wp, bp, sp, lp
 
 
@@ -368,11 +362,11 @@ def fpde_causal_conv(x, weight, bias=None, *, silu: bool = True, state=None, len
     what = "fpde_causal_conv"
     code, B, L, D, bs, ts, W, wp, bp, sp, lp = _conv_common(what, x, weight, bias, state, lengths)
     dev, dt = x.device, x.dtype
-    so = None if state_out is None else _dense(f"{what} state_out", state_out, (B, W - 1, D), dt, dev)
+    so = None if state_out is None else _dense(what, "state_out", state_out, (B, W - 1, D), dt, dev)
     if out is None:
         out = _empty(stream, (B, L, D), dt, dev)
     else:
-        _dense(f"{what} out", out, (B, L, D), dt, dev)
+        _dense(what, "out", out, (B, L, D), dt, dev)
     _call(what, ConvArgs(code, _CODES[weight.dtype], W, bool(silu), B, L, D, bs, ts, x.data_ptr(), wp, bp, sp, lp,
                          out.data_ptr(), so), stream)
     return out
@@ -382,7 +376,7 @@ def fpde_causal_conv_step(x, state, weight, bias=None, *, silu: bool = True, out
     """One level of ``fpde_causal_conv``: x [B, D]; ``state`` [B, taps - 1, D] is read
     and updated in place.  Returns y [B, D]."""
     what = "fpde_causal_conv_step"
-    code = _data(f"{what} x", x)
+    code = _data(what, "x", x)
     if x.dim() != 2 or not isinstance(weight, _Tensor) or weight.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
         raise ValueError(f"{what}: need x [batch, channels] with dense channels and weight [channels, taps]")
     dev, dt = x.device, x.dtype
@@ -391,10 +385,10 @@ def fpde_causal_conv_step(x, state, weight, bias=None, *, silu: bool = True, out
     if out is None:
         out = _empty_like(stream, x)
     else:
-        _dense(f"{what} out", out, x.shape, dt, dev)
-    wp = _param(f"{what} weight", weight, (D, W), dt, dev)
-    bp = None if bias is None else _dense(f"{what} bias", bias, (D,), weight.dtype, dev)
-    sp = _dense(f"{what} state", state, (B, W - 1, D), dt, dev)
+        _dense(what, "out", out, x.shape, dt, dev)
+    wp = _param(what, "weight", weight, (D, W), dt, dev)
+    bp = None if bias is None else _dense(what, "bias", bias, (D,), weight.dtype, dev)
+    sp = _dense(what, "state", state, (B, W - 1, D), dt, dev)
     _call("fpde_causal_conv", ConvArgs(code, _CODES[weight.dtype], W, bool(silu), B, 1, D, x.stride(0), D,
                                        x.data_ptr(), wp, bp, sp, None, out.data_ptr(), sp), stream)
     return out
@@ -406,10 +400,8 @@ def fpde_causal_conv_bwd(dy, x, weight, bias=None, *, silu: bool = True, state=N
     what = "fpde_causal_conv_bwd"
     code, B, L, D, bs, ts, W, wp, bp, sp, lp = _conv_common(what, x, weight, bias, state, lengths)
     dev, dt = x.device, x.dtype
-    _data(f"{what} dy", dy, dev, dt)
-    if dy.shape != x.shape:
-        raise ValueError(f"{what}: dy {tuple(dy.shape)} is not like x {tuple(x.shape)}")
-    _, _, _, dbs, dts = _levels(f"{what} dy", dy)
+    _like(what, "dy", dy, x)
+    _, _, _, dbs, dts = _levels(what, "dy", dy)
     dx = _empty(stream, (B, L, D), dt, dev)
     dw = _empty(stream, (D, W), weight.dtype, dev)
     db = None if bias is None else _empty(stream, (D,), weight.dtype, dev)
@@ -445,9 +437,9 @@ class CausalConv(torch.autograd.Function):
 
 def _scan_common(what, u, delta, A, B, C, D, z, delta_bias, softplus, state, lengths):
     """The arguments that both directions share: (head, inputs, dims)."""
-    code = _data(f"{what} u", u)
+    code = _data(what, "u", u)
     dev, dt = u.device, u.dtype
-    Bn, L, Dn, ubs, uts = _levels(f"{what} u", u)
+    Bn, L, Dn, ubs, uts = _levels(what, "u", u)
     if not isinstance(A, torch.Tensor) or A.dim() != 2:
         raise ValueError(f"{what} A: need [channels, states]")
     n = A.shape[1]
@@ -456,24 +448,23 @@ def _scan_common(what, u, delta, A, B, C, D, z, delta_bias, softplus, state, len
         if t is None:
             strides += [0, 0]
             continue
-        _data(f"{what} {name}", t, dev, dt)
-        if t.shape != u.shape:
-            raise ValueError(f"{what}: {name} {tuple(t.shape)} is not like u {tuple(u.shape)}")
-        strides += _levels(f"{what} {name}", t)[3:]
+        _like(what, name, t, u)
+        strides += _levels(what, name, t)[3:]
     groups = B.shape[2] if isinstance(B, torch.Tensor) and B.dim() == 4 else 1
     for name, t in (("B", B), ("C", C)):
-        _data(f"{what} {name}", t, dev, dt)
+        if not isinstance(t, _Tensor) or t.dtype is not dt or t.device != dev:
+            raise ValueError(f"{what} {name}: need a {dt} tensor on {dev}")
         if t.shape != (Bn, L, groups, n) and (groups > 1 or t.shape != (Bn, L, n)):
             raise ValueError(f"{what} {name}: need [batch, length, groups, states] (or without groups)")
         if (n > 1 and t.stride(-1) != 1) or (groups > 1 and t.stride(2) != n):
             raise ValueError(f"{what} {name}: groups and states have to be dense")
         strides += [t.stride(0), t.stride(1)]
     f32 = torch.float32
-    ptrs = [u.data_ptr(), delta.data_ptr(), _dense(f"{what} A", A, (Dn, n), f32, dev), B.data_ptr(), C.data_ptr(),
-            None if D is None else _dense(f"{what} D", D, (Dn,), f32, dev), None if z is None else z.data_ptr(),
-            None if delta_bias is None else _dense(f"{what} delta_bias", delta_bias, (Dn,), f32, dev),
-            None if state is None else _dense(f"{what} state", state, (Bn, Dn, n), f32, dev),
-            None if lengths is None else _dense(f"{what} lengths", lengths, (Bn,), torch.int32, dev)]
+    ptrs = [u.data_ptr(), delta.data_ptr(), _dense(what, "A", A, (Dn, n), f32, dev), B.data_ptr(), C.data_ptr(),
+            None if D is None else _dense(what, "D", D, (Dn,), f32, dev), None if z is None else z.data_ptr(),
+            None if delta_bias is None else _dense(what, "delta_bias", delta_bias, (Dn,), f32, dev),
+            None if state is None else _dense(what, "state", state, (Bn, Dn, n), f32, dev),
+            None if lengths is None else _dense(what, "lengths", lengths, (Bn,), torch.int32, dev)]
     return [code, n, groups, bool(softplus), Bn, L, Dn, *strides], ptrs, (Bn, L, Dn, groups, n)
 
 
@@ -491,11 +482,11 @@ def fpde_selective_scan(u, delta, A, B, C, *, D=None, z=None, delta_bias=None, s
     what = "fpde_selective_scan"
     head, ptrs, (Bn, L, Dn, _, n) = _scan_common(what, u, delta, A, B, C, D, z, delta_bias, softplus, state, lengths)
     dev, dt = u.device, u.dtype
-    so = None if state_out is None else _dense(f"{what} state_out", state_out, (Bn, Dn, n), torch.float32, dev)
+    so = None if state_out is None else _dense(what, "state_out", state_out, (Bn, Dn, n), torch.float32, dev)
     if out is None:
         out = _empty(stream, (Bn, L, Dn), dt, dev)
     else:
-        _dense(f"{what} out", out, (Bn, L, Dn), dt, dev)
+        _dense(what, "out", out, (Bn, L, Dn), dt, dev)
     a = ScanArgs(*head, *ptrs, out.data_ptr(), so, None, 0)
     if L > 1:
         _workspace(what, a, dev, stream)
@@ -509,7 +500,7 @@ def fpde_selective_step(state, u, delta, A, B, C, *, D=None, z=None, delta_bias=
     states] or [b, states]; ``state`` [b, channels, states] is read and updated in
     place.  Returns y [b, channels]."""
     what = "fpde_selective_step"
-    code = _data(f"{what} u", u)
+    code = _data(what, "u", u)
     if u.dim() != 2 or not isinstance(A, _Tensor) or A.dim() != 2:
         raise ValueError(f"{what}: need u [batch, channels] and A [channels, states]")
     dev, dt, f32 = u.device, u.dtype, _F32
@@ -521,12 +512,13 @@ def fpde_selective_step(state, u, delta, A, B, C, *, D=None, z=None, delta_bias=
         if t is None and name == "z":
             strides += (0, 0)
             continue
-        _data(f"{what} {name}", t, dev, dt)
-        if t.shape != u.shape or (Dn > 1 and t.stride(1) != 1):
-            raise ValueError(f"{what} {name}: need [batch, channels] like u, with dense channels")
+        _like(what, name, t, u)
+        if Dn > 1 and t.stride(1) != 1:
+            raise ValueError(f"{what} {name}: channels have to be dense")
         strides += (t.stride(0), Dn)
     for name, t in (("B", B), ("C", C)):
-        _data(f"{what} {name}", t, dev, dt)
+        if not isinstance(t, _Tensor) or t.dtype is not dt or t.device != dev:
+            raise ValueError(f"{what} {name}: need a {dt} tensor on {dev}")
         if t.shape != (Bn, groups, n) and (groups > 1 or t.shape != (Bn, n)):
             raise ValueError(f"{what} {name}: need [batch, groups, states] (or without groups)")
         if (n > 1 and t.stride(-1) != 1) or (groups > 1 and t.stride(1) != n):
@@ -535,13 +527,13 @@ def fpde_selective_step(state, u, delta, A, B, C, *, D=None, z=None, delta_bias=
     if out is None:
         out = _empty_like(stream, u)
     else:
-        _dense(f"{what} out", out, u.shape, dt, dev)
-    sp = _dense(f"{what} state", state, (Bn, Dn, n), f32, dev)
+        _dense(what, "out", out, u.shape, dt, dev)
+    sp = _dense(what, "state", state, (Bn, Dn, n), f32, dev)
     _call("fpde_selective_scan", ScanArgs(
         code, n, groups, bool(softplus), Bn, 1, Dn, *strides, u.data_ptr(), delta.data_ptr(),
-        _dense(f"{what} A", A, (Dn, n), f32, dev), B.data_ptr(), C.data_ptr(),
-        None if D is None else _dense(f"{what} D", D, (Dn,), f32, dev), None if z is None else z.data_ptr(),
-        None if delta_bias is None else _dense(f"{what} delta_bias", delta_bias, (Dn,), f32, dev), sp, None,
+        _dense(what, "A", A, (Dn, n), f32, dev), B.data_ptr(), C.data_ptr(),
+        None if D is None else _dense(what, "D", D, (Dn,), f32, dev), None if z is None else z.data_ptr(),
+        None if delta_bias is None else _dense(what, "delta_bias", delta_bias, (Dn,), f32, dev), sp, None,
         out.data_ptr(), sp, None, 0), stream)
     return out
 
@@ -558,10 +550,8 @@ def fpde_selective_scan_bwd(dy, u, delta, A, B, C, *, D=None, z=None, delta_bias
     head, ptrs, (Bn, L, Dn, groups, n) = _scan_common(what, u, delta, A, B, C, D, z, delta_bias, softplus, state,
                                                       lengths)
     dev, dt = u.device, u.dtype
-    _data(f"{what} dy", dy, dev, dt)
-    if dy.shape != u.shape:
-        raise ValueError(f"{what}: dy {tuple(dy.shape)} is not like u {tuple(u.shape)}")
-    dys = _levels(f"{what} dy", dy)[3:]
+    _like(what, "dy", dy, u)
+    dys = _levels(what, "dy", dy)[3:]
     f32 = torch.float32
     g = ScanGrads(_empty(stream, (Bn, L, Dn), dt, dev), _empty(stream, (Bn, L, Dn), dt, dev),
                   _empty(stream, (Dn, n), f32, dev), _empty(stream, B.shape, dt, dev), _empty(stream, C.shape, dt, dev),
@@ -600,14 +590,12 @@ class SelectiveScan(torch.autograd.Function):
 NS_COEFFS = (3.4445, -4.7750, 2.0315)
 
 
-def _matrices(what, ts, like=None, dtype=None):
+def _matrices(what, name, ts, like=None, dtype=None):
     """(tensors, host array of their pointers) of dense matrices of one shape, type and device."""
     ts = list(ts)
     t0 = ts[0] if like is None else like
     shape, dt, dev = t0.shape, dtype or t0.dtype, t0.device
-    for t in ts:
-        _dense(what, t, shape, dt, dev)
-    return ts, (_vp * len(ts))(*[t.data_ptr() for t in ts])
+    return ts, (_vp * len(ts))(*[_dense(what, name, t, shape, dt, dev) for t in ts])
 
 
 def fpde_orthogonalize(mats, *, steps: int = 5, coeffs=NS_COEFFS, eps: float = 1e-7, out=None, stream=None):
@@ -618,14 +606,14 @@ def fpde_orthogonalize(mats, *, steps: int = 5, coeffs=NS_COEFFS, eps: float = 1
     what = "fpde_orthogonalize"
     one = isinstance(mats, torch.Tensor)
     if one:
-        code = _data(what, mats)
+        code = _data(what, "input", mats)
         if mats.dim() < 2 or not mats.is_contiguous():
             raise ValueError(f"{what}: need a contiguous [..., m, n] tensor")
         dev, (m, n) = mats.device, mats.shape[-2:]
         if out is None:
             out = _empty(stream, mats.shape, mats.dtype, dev)
         else:
-            _dense(f"{what} out", out, mats.shape, mats.dtype, dev)
+            _dense(what, "out", out, mats.shape, mats.dtype, dev)
         count = mats.numel() // (m * n) if m * n else 0
         step = m * n * mats.element_size()
         gp, op = ((_vp * count)(*[t.data_ptr() + i * step for i in range(count)]) for t in (mats, out))
@@ -633,14 +621,14 @@ def fpde_orthogonalize(mats, *, steps: int = 5, coeffs=NS_COEFFS, eps: float = 1
         mats = list(mats)
         if not mats:
             return []
-        code = _data(what, mats[0])
+        code = _data(what, "input", mats[0])
         dev = mats[0].device
         if mats[0].dim() != 2:
             raise ValueError(f"{what}: need [m, n] matrices")
         (m, n), count = mats[0].shape, len(mats)
-        mats, gp = _matrices(what, mats)
+        mats, gp = _matrices(what, "input", mats)
         out = [_empty(stream, t.shape, t.dtype, dev) for t in mats] if out is None else out
-        out, op = _matrices(f"{what} out", out, mats[0])
+        out, op = _matrices(what, "out", out, mats[0])
         if len(out) != count:
             raise ValueError(f"{what}: {len(out)} outputs for {count} matrices")
     a = OrthoArgs(code, steps, count, m, n, *coeffs, eps, ctypes.cast(gp, _vp), ctypes.cast(op, _vp), None, 0)
@@ -663,13 +651,13 @@ def fpde_muon_step(weights, grads, momenta, *, lr: float, momentum: float = 0.95
     weights = list(weights)
     if not weights:
         return
-    code = _data(f"{what} weights", weights[0])
+    code = _data(what, "weights", weights[0])
     if weights[0].dim() != 2:
         raise ValueError(f"{what}: need [m, n] matrices")
     m, n = weights[0].shape
-    weights, wp = _matrices(f"{what} weights", weights)
-    grads, gp = _matrices(f"{what} grads", grads, weights[0])
-    momenta, mp = _matrices(f"{what} momenta", momenta, weights[0], torch.float32)
+    weights, wp = _matrices(what, "weights", weights)
+    grads, gp = _matrices(what, "grads", grads, weights[0])
+    momenta, mp = _matrices(what, "momenta", momenta, weights[0], torch.float32)
     if len(grads) != len(weights) or len(momenta) != len(weights):
         raise ValueError(f"{what}: {len(weights)} weights, {len(grads)} gradients, {len(momenta)} momenta")
     if scale is None:
