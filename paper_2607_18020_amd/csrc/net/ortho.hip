@@ -352,10 +352,12 @@ struct Half {
     int ld;
 };
 
-__device__ __forceinline__ void put_halves(float v, const Half& H, int64_t i) {
+// two neighbouring values of a row
+__device__ __forceinline__ void put_halves(float a, float b, const Half& H, int64_t i) {
     f16x2 hi, lo;
-    split2(v * kS, 0.f, hi, lo);
-    H.hi[i] = hi[0], H.lo[i] = lo[0];
+    split2(a * kS, b * kS, hi, lo);
+    *(f16x2*)(H.hi + i) = hi;
+    *(f16x2*)(H.lo + i) = lo;
 }
 
 // X0 in both orders, zeros in the padding.  64 x 64 tiles of X; 256 threads.
@@ -364,12 +366,6 @@ __global__ __launch_bounds__(256) void ortho_split_kernel(Mats M, const double* 
     __shared__ float tile[64][65];
     __shared__ double red[4];
     const int mat = (int)blockIdx.z, lane = (int)(threadIdx.x & 63), wave = (int)(threadIdx.x >> 6);
-    const double* q = part + mat * kNormBlocks + threadIdx.x;
-    double ss = wave_sum((q[0] + q[256]) + (q[512] + q[768]));
-    if (lane == 0) red[wave] = ss;
-    __syncthreads();
-    ss = (red[0] + red[1]) + (red[2] + red[3]);
-    const float inv = inv_norm(ss, M.eps);
     const int r0 = (int)blockIdx.y * 64, c0 = (int)blockIdx.x * 64;
     const int s = M.tall ? M.n : M.m, l = M.tall ? M.m : M.n;
     float g[16], m[16];
@@ -385,18 +381,29 @@ __global__ __launch_bounds__(256) void ortho_split_kernel(Mats M, const double* 
     };
     each([&](int h, int, int64_t k, bool) { g[h] = to_f32<T>(((const T*)M.g[mat])[k]); });
     if (M.muon) each([&](int h, int, int64_t k, bool) { m[h] = M.mom[mat][k]; });
+    // (the norm's sums come in while the elements are on their way)
+    const double* q = part + mat * kNormBlocks + threadIdx.x;
+    double ss = wave_sum((q[0] + q[256]) + (q[512] + q[768]));
+    if (lane == 0) red[wave] = ss;
+    __syncthreads();
+    ss = (red[0] + red[1]) + (red[2] + red[3]);
+    const float inv = inv_norm(ss, M.eps);
     each([&](int h, int i, int64_t, bool in) {
         (M.tall ? tile[lane][i] : tile[i][lane]) = in ? inv * update_of(M, g[h], m[h]) : 0.f;
     });
     __syncthreads();
-    for (int i = wave; i < 64; i += 4) {
-        const int64_t a = mat * X.step + (int64_t)(r0 + i) * X.ld + c0 + lane;
-        put_halves(tile[i][lane], X, a);
-        const int64_t b = mat * Xt.step + (int64_t)(c0 + i) * Xt.ld + r0 + lane;
-        put_halves(tile[lane][i], Xt, b);
+    // two columns a lane, two rows a wavefront
+    const int i0 = wave * 2 + (lane >> 5), j = (lane & 31) * 2;
+#pragma unroll
+    for (int h = 0; h < 8; ++h) {
+        const int i = i0 + h * 8;
+        put_halves(tile[i][j], tile[i][j + 1], X, mat * X.step + (int64_t)(r0 + i) * X.ld + c0 + j);
+        put_halves(tile[j][i], tile[j + 1][i], Xt, mat * Xt.step + (int64_t)(c0 + i) * Xt.ld + r0 + j);
     }
 }
 
+// KG groups of four wavefronts share the sum's length; each has NB operand tiles in LDS, NB - 1 of them on
+// their way.
 // S C = ca (S Z) + cp (S U) (S V)^T for [M][K] U and [N][K] V; C in both orders, or 1 / S of it into the
 // results (cp and ca hold that factor then).
 struct Prod {
@@ -433,19 +440,19 @@ __device__ __forceinline__ void tile_at(int i, int tm, int tn, bool sym, int* r,
 typedef const __attribute__((address_space(1))) void* gptr_t;
 typedef __attribute__((address_space(3))) void* lptr_t;
 
-template <int TILE, bool LAST, class T>
-__global__ __launch_bounds__(256) void ortho_product_kernel(Prod P, Mats M) {
+template <int TILE, int KG, int NB, bool LAST, class T>
+__global__ __launch_bounds__(256 * KG) void ortho_product_kernel(Prod P, Mats M) {
     constexpr int CH = TILE * 4;                       // 16-byte chunks of a TILE x 32 operand tile
     constexpr int W = TILE / 2, F = W / 32;            // a wavefront's share, in 32 x 32 tiles
     constexpr int STAGE = 4 * CH;                      // chunks: U hi, U lo, V hi, V lo
-    constexpr int NB = TILE == 64 ? 4 : 2;             // operand tiles in LDS, NB - 1 of them on their way
     constexpr int LOADS = 4 * CH / 256;                // a wavefront's loads a tile
     constexpr int PT = TILE + 4;                       // the result tile in float32: its pitch
-    constexpr int OUT = TILE * PT * 4;
-    constexpr int BYTES = NB * STAGE * 16 > OUT ? NB * STAGE * 16 : OUT;
+    constexpr int OUT = KG * TILE * PT * 4;
+    constexpr int RING = KG * NB * STAGE * 16, BYTES = RING > OUT ? RING : OUT;
     __shared__ __attribute__((aligned(16))) char lds[BYTES];
     const int lane = (int)(threadIdx.x & 63);
-    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6) & 3);
+    const int kg = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 8));
     // Workgroups go round the 8 XCDs in turn: each XCD takes a run of neighbouring tiles, which its L2 then
     // holds once, and not every eighth of all matrices.
     const int all = (int)gridDim.x, whole = all & ~7, id = (int)blockIdx.x;
@@ -466,13 +473,13 @@ __global__ __launch_bounds__(256) void ortho_product_kernel(Prod P, Mats M) {
             for (int i = 0; i < CH / 256; ++i) {
                 const int q0 = i * 256 + wave * 64, q = q0 + lane, row = q >> 2, ch = (q & 3) ^ ((row >> 2) & 3);
                 const f16* g = src[o] + (int64_t)row * (o < 2 ? P.U.ld : P.V.ld) + k + ch * 8;
-                __builtin_amdgcn_global_load_lds((gptr_t)g, (lptr_t)(lds + ((buf * 4 + o) * CH + q0) * 16), 16, 0,
+                __builtin_amdgcn_global_load_lds((gptr_t)g, (lptr_t)(lds + (((kg * NB + buf) * 4 + o) * CH + q0) * 16), 16, 0,
                                                  0);
             }
     };
     const int wr = (wave >> 1) * W, wc = (wave & 1) * W, r = lane & 31, kh = lane >> 5;
     auto operand = [&](int o, int buf, int row, int ch) {
-        return *(const f16x8*)(lds + ((buf * 4 + o) * CH + row * 4 + (ch ^ ((row >> 2) & 3))) * 16);
+        return *(const f16x8*)(lds + (((kg * NB + buf) * 4 + o) * CH + row * 4 + (ch ^ ((row >> 2) & 3))) * 16);
     };
     // A sum's three products in turn would each wait for the one before: with four tiles a wavefront
     // they are four instructions apart, with one tile each has a sum of its own.
@@ -486,18 +493,23 @@ __global__ __launch_bounds__(256) void ortho_product_kernel(Prod P, Mats M) {
             for (int j = 0; j < F; ++j)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) acc[p][i][j][e] = 0.f;
+    // Group kg of the workgroup's wavefronts has every KG-th tile of 32 k; all go the same number of rounds,
+    // since they meet at the barriers.
+    constexpr int STEP = 32 * KG;
+    const int mine = kg * 32;
 #pragma unroll
     for (int i = 0; i < NB - 1; ++i)
-        if (i * 32 < P.K) fetch(i * 32, i);
+        if (i * STEP + mine < P.K) fetch(i * STEP + mine, i);
     int buf = 0;
-    for (int k = 0; k < P.K; k += 32, buf = buf + 1 == NB ? 0 : buf + 1) {
+    for (int k = 0; k < P.K; k += STEP, buf = buf + 1 == NB ? 0 : buf + 1) {
         // This wavefront's part of the tile is in LDS when all but the later tiles' loads have arrived;
         // past the barrier everyone's is, and nobody reads the tile before any more.
-        if (k + (NB - 2) * 32 < P.K)
+        if (k + (NB - 2) * STEP + mine < P.K)
             asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((NB - 2) * LOADS) : "memory");
         else
             asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (k + (NB - 1) * 32 < P.K) fetch(k + (NB - 1) * 32, buf == 0 ? NB - 1 : buf - 1);
+        if (k + (NB - 1) * STEP + mine < P.K) fetch(k + (NB - 1) * STEP + mine, buf == 0 ? NB - 1 : buf - 1);
+        if (KG > 1 && k + mine >= P.K) continue;
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
             f16x8 uh[F], ul[F], vh[F], vl[F];
@@ -519,24 +531,27 @@ __global__ __launch_bounds__(256) void ortho_product_kernel(Prod P, Mats M) {
         }
     }
     // The tile by way of LDS, so that both orders are written along their rows, 8 elements a lane.
-    constexpr int IT = TILE * TILE / 8 / 256;
+    constexpr int THREADS = 256 * KG < TILE * TILE / 8 ? 256 * KG : TILE * TILE / 8;  // of the epilogue
+    constexpr int IT = TILE * TILE / 8 / THREADS;
+    const bool writer = (int)threadIdx.x < THREADS;
     f16x8 zh[IT], zl[IT];
-    auto spot = [&](int it, int* row, int* col) {
-        const int q = it * 256 + (int)threadIdx.x;
+    auto place = [&](int it, int* row, int* col) {
+        const int q = it * THREADS + (writer ? (int)threadIdx.x : 0);
         *row = q / (TILE / 8), *col = q % (TILE / 8) * 8;
     };
     if (P.Z.hi) {
 #pragma unroll
         for (int it = 0; it < IT; ++it) {
             int row, col;
-            spot(it, &row, &col);
+            place(it, &row, &col);
             const int64_t z = mat * P.Z.step + (int64_t)(tr * TILE + row) * P.Z.ld + tc * TILE + col;
             zh[it] = *(const f16x8*)(P.Z.hi + z);
             zl[it] = *(const f16x8*)(P.Z.lo + z);
         }
     }
     __syncthreads();
-    float* t = (float*)lds;
+    float* const tile = (float*)lds;
+    float* t = tile + kg * (TILE * PT);
 #pragma unroll
     for (int i = 0; i < F; ++i)
 #pragma unroll
@@ -556,14 +571,18 @@ __global__ __launch_bounds__(256) void ortho_product_kernel(Prod P, Mats M) {
         *(f16x8*)(H.lo + c) = lo;
     };
     const bool both = LAST ? M.tall : !(P.sym && tr == tc);
+    t = tile;
 #pragma unroll
     for (int it = 0; it < IT; ++it) {
+        if (!writer) break;
         int row, col;
-        spot(it, &row, &col);
+        place(it, &row, &col);
         float v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             v[e] = t[row * PT + col + e];
+#pragma unroll
+            for (int g = 1; g < KG; ++g) v[e] += t[g * (TILE * PT) + row * PT + col + e];
             if (P.Z.hi) v[e] = fmaf(P.ca, (float)zh[it][e] + (float)zl[it][e], v[e]);
         }
         if (both) {
@@ -581,8 +600,9 @@ __global__ __launch_bounds__(256) void ortho_product_kernel(Prod P, Mats M) {
     __syncthreads();
 #pragma unroll
     for (int it = 0; it < IT; ++it) {
+        if (!writer) break;
         // 16 neighbouring columns and 4 groups of rows a wavefront: few lanes meet in a bank
-        const int q = it * 256 + (int)threadIdx.x, col = q % 16 + q / (16 * (TILE / 8)) * 16;
+        const int q = it * THREADS + (int)threadIdx.x, col = q % 16 + q / (16 * (TILE / 8)) * 16;
         const int row = q / 16 % (TILE / 8) * 8, grow = tr * TILE + row, gcol = tc * TILE + col;
         float v[8];
 #pragma unroll
@@ -665,12 +685,17 @@ int run_large(const Mats& M, const OrthoPlan& p, int count, int steps, float ca,
                    M, part, X[0], Xt[0]);
     const int ts = (int)(p.sp / p.tile), tl = (int)(p.lp / p.tile), tri = ts * (ts + 1) / 2;
     auto product = [&](const Prod& P, bool last) {
-        const dim3 g((unsigned)(P.tiles * count)), b(256);
+        const dim3 g((unsigned)(P.tiles * count));
         if (p.tile == 128)
-            return last ? launch(ortho_product_kernel<128, true, T>, g, b, s, P, M)
-                        : launch(ortho_product_kernel<128, false, float>, g, b, s, P, M);
-        return last ? launch(ortho_product_kernel<64, true, T>, g, b, s, P, M)
-                    : launch(ortho_product_kernel<64, false, float>, g, b, s, P, M);
+            return last ? launch(ortho_product_kernel<128, 1, 2, true, T>, g, dim3(256), s, P, M)
+                        : launch(ortho_product_kernel<128, 1, 2, false, float>, g, dim3(256), s, P, M);
+        // Up to one workgroup for every compute unit: four times the wavefronts share the sum's length, as
+        // a single wavefront a SIMD waits for its own reads and products in turn.
+        if (g.x <= 256)
+            return last ? launch(ortho_product_kernel<64, 4, 2, true, T>, g, dim3(1024), s, P, M)
+                        : launch(ortho_product_kernel<64, 4, 2, false, float>, g, dim3(1024), s, P, M);
+        return last ? launch(ortho_product_kernel<64, 1, 4, true, T>, g, dim3(256), s, P, M)
+                    : launch(ortho_product_kernel<64, 1, 4, false, float>, g, dim3(256), s, P, M);
     };
     const Half none{nullptr, nullptr, 0, 0};
     for (int i = 0; i < steps && r == FPDE_OK; ++i) {
