@@ -123,8 +123,8 @@ int fpde_rms_norm_bwd(const fpde_norm_bwd_args* a, void* stream);
  * taps - 1 levels of each sequence, state included where it is shorter.  A single
  * level (length 1) with state_out = state is the step of a rollout.
  *
- * Limits: 2 <= taps <= 4, 1 <= channels <= 2^20, 0 <= batch, 0 <= length < 2^31,
- * batch * length <= 2^40. */
+ * Limits: 2 <= taps <= 4, 1 <= channels <= 2^20, 0 <= batch <= 2^34, 0 <= length <
+ * 2^31 - 256, batch * length <= 2^34. */
 typedef struct fpde_conv_args {
     int32_t dtype;            /* x, y, state, state_out */
     int32_t weight_dtype;     /* weight and bias: FPDE_F32, or dtype */
@@ -183,8 +183,8 @@ int fpde_causal_conv_bwd(const fpde_conv_bwd_args* a, void* stream);
  * are float32 whatever the data's type.
  *
  * Limits: 1 <= states <= 32 (FPDE_ERR_UNSUPPORTED above), groups divides channels,
- * 1 <= channels <= 2^20, 0 <= batch, 0 <= length < 2^31 - 256,
- * batch * length <= 2^40. */
+ * 1 <= channels <= 2^20, 0 <= batch <= 2^34, 0 <= length < 2^31 - 256,
+ * batch * length <= 2^34. */
 typedef struct fpde_scan_args {
     int32_t dtype;            /* u, delta, B, C, z, y */
     int32_t states, groups;

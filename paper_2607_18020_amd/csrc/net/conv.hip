@@ -242,7 +242,7 @@ __global__ __launch_bounds__(64) void conv_bwd_kernel(ConvP P) {
 // ---------------------------------------------------------------------------
 // Host side.
 
-constexpr int64_t kMaxChannels = 1 << 20, kMaxLevels = (int64_t)1 << 40;
+constexpr int64_t kMaxChannels = 1 << 20, kMaxLevels = (int64_t)1 << 34;
 // Wavefronts of a launch before they loop over chunks.  The backward's partial
 // sums grow with them.
 constexpr int64_t kFwdWaves = 1 << 20, kBwdWaves = 4096;

@@ -493,7 +493,10 @@ int check_norm(int dtype, int wdtype, int64_t rows, int64_t width, double eps) {
     return FPDE_OK;
 }
 
-bool stride_ok(int64_t stride, int64_t width) { return stride >= width && stride <= (int64_t)1 << 40; }
+// (rows * stride elements stay far below 2^63 bytes)
+bool stride_ok(int64_t stride, int64_t width, int64_t rows) {
+    return stride >= width && stride <= ((int64_t)1 << 60) / (rows < 1 ? 1 : rows);
+}
 
 int64_t bwd_blocks(int64_t rows, int rows_per_block) {
     const int64_t n = cdiv(rows, rows_per_block);
@@ -515,7 +518,7 @@ extern "C" int fpde_rms_norm(const fpde_norm_args* a, void* stream) {
     const bool f8 = a->out_dtype == FPDE_F8E4M3;
     if (!f8 && a->out_dtype != a->dtype) return FPDE_ERR_UNSUPPORTED;
     if (f8 && a->group != 128 && a->group != 0) return FPDE_ERR_UNSUPPORTED;
-    if (!stride_ok(a->x_stride, a->width) || (a->residual && !stride_ok(a->residual_stride, a->width)))
+    if (!stride_ok(a->x_stride, a->width, a->rows) || (a->residual && !stride_ok(a->residual_stride, a->width, a->rows)))
         return FPDE_ERR_SHAPE;
     if (a->rows == 0) return FPDE_OK;
     if (!a->x || !a->y || (f8 && !a->scales)) return FPDE_ERR_ARG;
@@ -572,8 +575,8 @@ extern "C" int fpde_rms_norm_bwd(const fpde_norm_bwd_args* a, void* stream) {
     if (!a) return FPDE_ERR_ARG;
     int st = check_norm(a->dtype, a->weight_dtype, a->rows, a->width, a->eps);
     if (st != FPDE_OK) return st;
-    if (!stride_ok(a->dy_stride, a->width) || !stride_ok(a->sum_stride, a->width) ||
-        (a->dsum && !stride_ok(a->dsum_stride, a->width)))
+    if (!stride_ok(a->dy_stride, a->width, a->rows) || !stride_ok(a->sum_stride, a->width, a->rows) ||
+        (a->dsum && !stride_ok(a->dsum_stride, a->width, a->rows)))
         return FPDE_ERR_SHAPE;
     if (a->rows > 0 && (!a->dy || !a->sum || !a->ds)) return FPDE_ERR_ARG;
     const int64_t need = fpde_rms_norm_bwd_workspace(a);

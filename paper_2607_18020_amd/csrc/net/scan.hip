@@ -819,7 +819,7 @@ __global__ __launch_bounds__(256) void scan_bc_kernel(ScanP P, int ns, T* dB, T*
 // ---------------------------------------------------------------------------
 // Host side.
 
-constexpr int64_t kMaxChannels = 1 << 20, kMaxLevels = (int64_t)1 << 40;
+constexpr int64_t kMaxChannels = 1 << 20, kMaxLevels = (int64_t)1 << 34;
 
 int states_of(int states) { return states <= 4 ? 4 : states <= 8 ? 8 : states <= 16 ? 16 : 32; }
 constexpr int kBlock = 8;  // levels between saved states in the backward

@@ -28,9 +28,9 @@ from collections import namedtuple
 from typing import Optional
 
 import torch
+from torch.autograd.function import once_differentiable
 
-from . import binding
-from .binding import FPDE_OK, FpdeError, _raw_stream, _stream, _used_on
+from .binding import FPDE_OK, FpdeError, _raw_stream, _stream
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libfpde_net.so")
@@ -145,9 +145,11 @@ def _workspace(name, args, dev, stream):
     if n < 0:
         raise FpdeError(n, name)
     if n:
-        ws = torch.empty(n, dtype=torch.uint8, device=dev)
-        if stream is not None:
-            _used_on(stream, ws)
+        if stream is None:
+            ws = torch.empty(n, dtype=torch.uint8, device=dev)
+        else:  # (memory of the stream that uses it, and of no other)
+            with torch.cuda.stream(stream):
+                ws = torch.empty(n, dtype=torch.uint8, device=dev)
         args.workspace, args.workspace_bytes = ws.data_ptr(), n
 
 
@@ -225,20 +227,22 @@ def _levels(what, name, t):
 
 
 def _empty(stream, shape, dtype, dev):
-    t = torch.empty(shape, dtype=dtype, device=dev)
-    if stream is not None:
-        _used_on(stream, t)
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    # Written on `stream` and then the caller's: memory that `stream` may use now (what the current
+    # stream has freed may still be in its queued work), not handed out again before the current one is done.
+    here = torch.cuda.current_stream()
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=dev)
+    t.record_stream(here)
     return t
 
 
 def _empty_like(stream, x, dtype=None):
     """A dense tensor like x."""
-    if not x.is_contiguous():
+    if stream is not None or not x.is_contiguous():
         return _empty(stream, x.shape, dtype or x.dtype, x.device)
-    t = torch.empty_like(x) if dtype is None else torch.empty_like(x, dtype=dtype)
-    if stream is not None:
-        _used_on(stream, t)
-    return t
+    return torch.empty_like(x) if dtype is None else torch.empty_like(x, dtype=dtype)
 
 
 # ---------------------------------------------------------------------------
@@ -327,6 +331,7 @@ class RmsNorm(torch.autograd.Function):
         return y, (s if residual is not None else s.view_as(s))
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy, dsum):
         s, weight = ctx.saved_tensors
         dy = torch.zeros_like(s) if dy is None else dy.to(s.dtype).contiguous()
@@ -425,6 +430,7 @@ class CausalConv(torch.autograd.Function):
         return fpde_causal_conv(x, weight, bias, silu=silu, state=state, lengths=lengths)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x, weight, bias, state, lengths = ctx.saved_tensors
         dx, dw, db = fpde_causal_conv_bwd(dy.contiguous(), x, weight, bias, silu=ctx.silu, state=state,
@@ -445,7 +451,7 @@ def _scan_common(what, u, delta, A, B, C, D, z, delta_bias, softplus, state, len
     n = A.shape[1]
     strides = [ubs, uts]
     for name, t in (("delta", delta), ("z", z)):
-        if t is None:
+        if t is None and name == "z":
             strides += [0, 0]
             continue
         _like(what, name, t, u)
@@ -577,6 +583,7 @@ class SelectiveScan(torch.autograd.Function):
                                    lengths=lengths)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         u, delta, A, B, C, D, z, bias, state, lengths = ctx.saved_tensors
         g = fpde_selective_scan_bwd(dy.contiguous(), u, delta, A, B, C, D=D, z=z, delta_bias=bias,
@@ -681,6 +688,15 @@ class Muon(torch.optim.Optimizer):
             for p in group["params"]:
                 if p.dim() != 2:
                     raise ValueError(f"Muon: parameters are matrices, got shape {tuple(p.shape)}")
+
+    def load_state_dict(self, state_dict):
+        """As the base class does, but momenta stay float32 whatever the parameters' type."""
+        super().load_state_dict(state_dict)
+        for group, saved in zip(self.param_groups, state_dict["param_groups"]):
+            for p, key in zip(group["params"], saved["params"]):
+                kept = state_dict["state"].get(key)
+                if kept is not None and "momentum" in kept:
+                    self.state[p]["momentum"] = kept["momentum"].detach().to(device=p.device, dtype=_F32, copy=True)
 
     @torch.no_grad()
     def step(self, closure=None):

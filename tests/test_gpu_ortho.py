@@ -165,3 +165,24 @@ def test_streams_and_graph(N):
             torch.cuda.synchronize()
             N.fpde_muon_step(w2.unbind(0), g.unbind(0), mom2.unbind(0), lr=0.1)
             assert torch.equal(w, w2) and torch.equal(mom, mom2)
+
+
+def test_momenta_of_16_bit_weights_survive_a_checkpoint(N):
+    gen = torch.Generator().manual_seed(4)
+    ps = [torch.nn.Parameter(R.randn(gen, 40, 24, dtype=torch.bfloat16).cuda()) for _ in range(2)]
+    opt = N.Muon(ps, lr=0.1)
+    for p in ps:
+        p.grad = R.randn(gen, 40, 24, dtype=torch.bfloat16).cuda()
+    opt.step()
+    kept = opt.state_dict()
+    other = [torch.nn.Parameter(p.detach().clone()) for p in ps]
+    again = N.Muon(other, lr=0.1)
+    again.load_state_dict(kept)
+    for p, q in zip(ps, other):
+        m = again.state[q]["momentum"]
+        assert m.dtype is torch.float32 and torch.equal(m, opt.state[p]["momentum"])
+        assert m.data_ptr() != opt.state[p]["momentum"].data_ptr()
+        q.grad = p.grad.clone()
+    opt.step(), again.step()
+    for p, q in zip(ps, other):
+        assert torch.equal(p, q)

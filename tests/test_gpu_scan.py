@@ -305,3 +305,52 @@ def test_autograd_and_differences(N):
         assert abs((f[0] - f[1]) / (2 * h) - want) <= 600 * h * h * 100 / 6 + 600 * 16 * 2.0 ** -24 / h, k
     with pytest.raises(ValueError):
         N.SelectiveScan.apply(*[leaf[k] for k in NAMES], True, c["state"].clone().requires_grad_(), None)
+
+
+def test_refusals(N):
+    t = inputs(2, 6, 8, 4, 1, torch.float32)
+    c = cuda(t)
+    args, opts = call(N, c)
+    u, delta, A, B, C = args
+    for bad, match in (((u, None, A, B, C), "delta"), ((u, delta.half(), A, B, C), "delta"),
+                       ((u, delta, A.double(), B, C), "A"), ((u, delta, A, B[:, :5], C), "B"),
+                       ((u, delta, A, B, C.bfloat16()), "C"), ((u[:, :, ::2], delta, A, B, C), "u|delta|channels"),
+                       ((u, delta, A[:, :2].t(), B, C), "A|B")):
+        with pytest.raises(ValueError, match=match):
+            N.fpde_selective_scan(*bad, **opts)
+    for name, bad in (("state", c["state"][:1]), ("lengths", c["lengths"].long()), ("D", c["D"][:3]), ("z", c["z"][:1]),
+                      ("delta_bias", c["bias"].half())):
+        with pytest.raises(ValueError, match=name):
+            N.fpde_selective_scan(*args, **dict(opts, **{name: bad}))
+    with pytest.raises(ValueError, match="dy"):
+        N.fpde_selective_scan_bwd(c["dy"][:1], *args, **opts)
+    with pytest.raises(N.FpdeError):  # levels that overlap
+        N.fpde_selective_scan(u[:, :1].expand(2, 6, 8), delta, A, B, C)
+    with pytest.raises(N.FpdeError):  # more states than the kernels hold
+        N.fpde_selective_scan(u, delta, torch.zeros(8, 33, device="cuda"), torch.zeros(2, 6, 33, device="cuda"),
+                              torch.zeros(2, 6, 33, device="cuda"))
+    with pytest.raises(N.FpdeError):  # the output over an input
+        N.fpde_selective_scan(u, delta, A, B, C, out=u)
+    # a second derivative is refused, not wrong
+    leaf = u.clone().requires_grad_()
+    g = torch.autograd.grad(N.SelectiveScan.apply(leaf, delta, A, B, C).pow(2).sum(), leaf, create_graph=True)[0]
+    with pytest.raises(RuntimeError):
+        g.sum().backward()
+
+
+def test_call_on_another_stream_owns_its_memory(N):
+    """Results and workspace of a call on a side stream come from that stream's memory: what the current stream
+    has just freed, but still has queued work on, is not written to."""
+    t = cuda(inputs(1, 600, 64, 16, 1, torch.float32))
+    args, opts = call(N, t)
+    ref = N.fpde_selective_scan(*args, **opts)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        x = torch.ones(1 << 24, device="cuda")
+        for _ in range(20):
+            x = x * 1.0  # (queued, its inputs freed at once)
+        got = N.fpde_selective_scan(*args, stream=side, **opts)
+        torch.cuda.current_stream().wait_stream(side)
+        assert torch.equal(got, ref)
+        assert bool((x == 1).all())

@@ -161,6 +161,7 @@ def test_norm_validation(N):
                      (dict(out_dtype=3, group=64, scales=addr(5)), UNSUPPORTED), (dict(out_dtype=3), ARG),
                      (dict(rows=-1), SHAPE), (dict(rows=(1 << 40) + 1), SHAPE), (dict(width=0), SHAPE),
                      (dict(width=(1 << 20) + 1), SHAPE), (dict(x_stride=63), SHAPE), (dict(residual_stride=10), SHAPE),
+                     (dict(rows=1 << 30, x_stride=1 << 31), SHAPE),
                      (dict(eps=-1e-9), COEFF), (dict(eps=float("nan")), COEFF), (dict(eps=float("inf")), COEFF),
                      (dict(x=None), ARG), (dict(y=None), ARG), (dict(x=addr(0, 1)), ALIGN), (dict(y=addr(3, 1)), ALIGN),
                      (dict(weight=addr(2, 2)), ALIGN), (dict(y=addr(0)), ARG), (dict(y=addr(1, 64)), ARG),
@@ -185,7 +186,7 @@ def test_conv_validation(N):
     f = "fpde_causal_conv"
     for kw, want in ((dict(taps=1), UNSUPPORTED), (dict(taps=5), UNSUPPORTED), (dict(silu=2), ARG), (dict(channels=0), SHAPE),
                      (dict(channels=(1 << 20) + 1), SHAPE), (dict(batch=-1), SHAPE), (dict(length=1 << 31), SHAPE),
-                     (dict(batch=1 << 38, length=1 << 10), SHAPE), (dict(x_time_stride=7), SHAPE),
+                     (dict(batch=1 << 30, length=1 << 10), SHAPE), (dict(batch=(1 << 34) + 1, length=0), SHAPE), (dict(x_time_stride=7), SHAPE),
                      (dict(x_batch_stride=-1), SHAPE), (dict(x=None), ARG), (dict(weight=None), ARG), (dict(y=None), ARG),
                      (dict(y=addr(0)), ARG), (dict(state_out=addr(3, 4)), ARG), (dict(lengths=addr(4, 2)), ALIGN),
                      (dict(batch=0), OK), (dict(length=0, state_out=None, x=None, y=None), OK)):
