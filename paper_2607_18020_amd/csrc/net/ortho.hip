@@ -410,6 +410,7 @@ struct Prod {
     Half U, V, Z, C, Ct;
     int tm, tn, tiles, K;  // tiles over the rows and columns of C, and of a matrix; the sum's length, 32 n
     int sym;             // C is square and symmetric: tiles on and above the diagonal, Ct = C
+    int first, quarters;  // the first tile of this launch; whether a tile's quarters are four workgroups'
     float ca, cp;
 };
 
@@ -456,10 +457,15 @@ __global__ __launch_bounds__(256 * KG) void ortho_product_kernel(Prod P, Mats M)
     // Workgroups go round the 8 XCDs in turn: each XCD takes a run of neighbouring tiles, which its L2 then
     // holds once, and not every eighth of all matrices.
     const int all = (int)gridDim.x, whole = all & ~7, id = (int)blockIdx.x;
-    const int at = id < whole ? (id & 7) * (whole >> 3) + (id >> 3) : id;
+    const int own = id < whole ? (id & 7) * (whole >> 3) + (id >> 3) : id;
+    const int at = P.first + (P.quarters ? own >> 2 : own);
     const int mat = at / P.tiles;
     int tr, tc;
     tile_at(at - mat * P.tiles, P.tm, P.tn, P.sym, &tr, &tc);
+    if (P.quarters) {
+        tr = tr * 2 + (own >> 1 & 1), tc = tc * 2 + (own & 1);
+        if (P.sym && tr > tc) return;
+    }
     const f16* src[4] = {P.U.hi + mat * P.U.step + (int64_t)tr * TILE * P.U.ld,
                          P.U.lo + mat * P.U.step + (int64_t)tr * TILE * P.U.ld,
                          P.V.hi + mat * P.V.step + (int64_t)tc * TILE * P.V.ld,
@@ -618,6 +624,9 @@ __global__ __launch_bounds__(256 * KG) void ortho_product_kernel(Prod P, Mats M)
 // ---------------------------------------------------------------------------
 // Host side.
 
+constexpr unsigned kUnits = 256;  // compute units
+constexpr unsigned kTail = 64;
+
 // Bytes of workspace that a batch of large matrices may take together.
 constexpr int64_t kBatchBytes = (int64_t)1 << 30;
 
@@ -637,10 +646,11 @@ OrthoPlan plan(int64_t count, int64_t m, int64_t n) {
               : p.l <= 128         ? 128 : 0;
     p.batch = kMaxCount, p.bytes = 0, p.tile = 0, p.sp = p.lp = 0;
     if (p.small) return p;
-    // Tiles of 128 need half the reads of 64 a flop, but only where there are enough of them for
-    // every compute unit.
+    // Tiles of 128 need half the reads of 64 a flop, but only where they are enough for half of the
+    // compute units.  Five steps, tiles of 128 / 64: one 2048 x 2048 matrix (136 tiles) 945 / 980 us, two of
+    // 1536 x 1536 (156) 880 / 860 us, one of 2560 x 2560 (210) 1480 / 1950 us, one of 1536 x 1536 (78) 732 / 523 us.
     const int64_t t = cdiv(p.s, 128);
-    p.tile = t * (t + 1) / 2 * (count < 1 ? 1 : count) >= 256 ? 128 : 64;
+    p.tile = t * (t + 1) / 2 * (count < 1 ? 1 : count) >= kUnits / 2 ? 128 : 64;
     p.sp = cdiv(p.s, p.tile) * p.tile, p.lp = cdiv(p.l, p.tile) * p.tile;
     // X and X^T twice (a step reads one and writes the other), A, B: hi and lo of each
     const int64_t each = (4 * p.sp * p.lp + 2 * p.sp * p.sp) * 4;
@@ -684,28 +694,40 @@ int run_large(const Mats& M, const OrthoPlan& p, int count, int steps, float ca,
         r = launch(ortho_split_kernel<T>, dim3((unsigned)(p.lp / 64), (unsigned)(p.sp / 64), count), dim3(256), s,
                    M, part, X[0], Xt[0]);
     const int ts = (int)(p.sp / p.tile), tl = (int)(p.lp / p.tile), tri = ts * (ts + 1) / 2;
-    auto product = [&](const Prod& P, bool last) {
-        const dim3 g((unsigned)(P.tiles * count));
-        if (p.tile == 128)
-            return last ? launch(ortho_product_kernel<128, 1, 2, true, T>, g, dim3(256), s, P, M)
-                        : launch(ortho_product_kernel<128, 1, 2, false, float>, g, dim3(256), s, P, M);
+    auto product = [&](Prod P, bool last) {
+        dim3 g((unsigned)(P.tiles * count));
+        P.first = P.quarters = 0;
+        if (p.tile == 128) {
+            // The last few tiles past a multiple of the compute units would be a round that few of them
+            // share: their quarters go to as many, in a launch of their own.  Five steps with / without:
+            // 4096 x 4096 (528 tiles) 4767 / 5194 us, 3000 x 3000 (300) 2371 / 2585 us.  With up to 128 tiles
+            // so, 3400 x 3400 (378) would go from 3012 to 3175 us.
+            const unsigned rest = g.x > 256 && g.x % 256 <= kTail ? g.x % 256 : 0;
+            g.x -= rest;
+            const int r = last ? launch(ortho_product_kernel<128, 1, 2, true, T>, g, dim3(256), s, P, M)
+                               : launch(ortho_product_kernel<128, 1, 2, false, float>, g, dim3(256), s, P, M);
+            if (rest == 0 || r != FPDE_OK) return r;
+            P.first = (int)g.x, P.quarters = 1;
+            g.x = rest * 4;
+        }
         // Up to one workgroup for every compute unit: four times the wavefronts share the sum's length, as
-        // a single wavefront a SIMD waits for its own reads and products in turn.
-        if (g.x <= 256)
+        // a single wavefront a SIMD waits for its own reads and products in turn.  Five steps with / without:
+        // one 1024 x 1024 matrix 229 / 242 us; with it up to 512 workgroups too, two of them 427 and not 347.
+        if (g.x <= kUnits)
             return last ? launch(ortho_product_kernel<64, 4, 2, true, T>, g, dim3(1024), s, P, M)
                         : launch(ortho_product_kernel<64, 4, 2, false, float>, g, dim3(1024), s, P, M);
-        return last ? launch(ortho_product_kernel<64, 1, 4, true, T>, g, dim3(256), s, P, M)
-                    : launch(ortho_product_kernel<64, 1, 4, false, float>, g, dim3(256), s, P, M);
+        return last ? launch(ortho_product_kernel<64, 1, 2, true, T>, g, dim3(256), s, P, M)
+                    : launch(ortho_product_kernel<64, 1, 2, false, float>, g, dim3(256), s, P, M);
     };
     const Half none{nullptr, nullptr, 0, 0};
     for (int i = 0; i < steps && r == FPDE_OK; ++i) {
         const int o = i & 1;
         const bool last = i + 1 == steps;
-        r = product(Prod{X[o], X[o], none, A, A, ts, ts, tri, (int)p.lp, 1, 0.f, kInvS}, false);
-        if (r == FPDE_OK) r = product(Prod{A, A, A, B, B, ts, ts, tri, (int)p.sp, 1, cb, cc * kInvS}, false);
+        r = product(Prod{X[o], X[o], none, A, A, ts, ts, tri, (int)p.lp, 1, 0, 0, 0.f, kInvS}, false);
+        if (r == FPDE_OK) r = product(Prod{A, A, A, B, B, ts, ts, tri, (int)p.sp, 1, 0, 0, cb, cc * kInvS}, false);
         if (r == FPDE_OK)
-            r = last ? product(Prod{B, Xt[o], X[o], none, none, ts, tl, ts * tl, (int)p.sp, 0, ca * kInvS, kInvSS}, true)
-                     : product(Prod{B, Xt[o], X[o], X[o ^ 1], Xt[o ^ 1], ts, tl, ts * tl, (int)p.sp, 0, ca, kInvS}, false);
+            r = last ? product(Prod{B, Xt[o], X[o], none, none, ts, tl, ts * tl, (int)p.sp, 0, 0, 0, ca * kInvS, kInvSS}, true)
+                     : product(Prod{B, Xt[o], X[o], X[o ^ 1], Xt[o ^ 1], ts, tl, ts * tl, (int)p.sp, 0, 0, 0, ca, kInvS}, false);
     }
     return r;
 }

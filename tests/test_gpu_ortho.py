@@ -186,3 +186,19 @@ def test_momenta_of_16_bit_weights_survive_a_checkpoint(N):
     opt.step(), again.step()
     for p, q in zip(ps, other):
         assert torch.equal(p, q)
+
+
+@pytest.mark.parametrize("count,m,n", [(26, 500, 300), (26, 300, 500), (1, 1930, 2050), (2, 2040, 1925)])
+def test_quarters_of_the_last_tiles(N, count, m, n):
+    """Tiles past a multiple of the compute units, in the symmetric products, the steps' and the last one."""
+    print(f"case muon {count} of {m} x {n}", flush=True)
+    g = torch.stack([matrix(m, n, s, torch.bfloat16) for s in range(count)])
+    o = N.fpde_orthogonalize(g.cuda(), steps=3)
+    gen = torch.Generator().manual_seed(11)
+    w = R.randn(gen, count, m, n)
+    wc, mc = w.cuda(), torch.zeros(count, m, n, device="cuda")
+    N.fpde_muon_step(wc.unbind(0), g.float().cuda().unbind(0), mc.unbind(0), lr=0.05, momentum=0.9, steps=3)
+    for i in {0, count // 2, count - 1}:
+        r = R.orthogonalize(g[i].cuda().double(), 3, CO, 1e-7).cpu()
+        near("orthogonalize", o[i], r)
+        near("weight", wc[i], w[i].double() - 0.05 * max(1.0, m / n) ** 0.5 * r)
