@@ -13,6 +13,9 @@
 // begin earlier, and what two lanes own they write with the same values.  The backward
 // recomputes p from x instead of reading it, and runs W - 1 levels past its chunk for
 // the dp that dx needs there.
+//
+// Measured, 256 x 128 x 512 bf16, 4 taps: forward 17 us (4.0 TB/s), backward 34 and 5 for
+// the partial sums (3.0 TB/s); with 8 channels a lane both together 151 and not 57 us.
 #include "net_common.hpp"
 
 using namespace fpde_net;
@@ -244,11 +247,12 @@ __global__ __launch_bounds__(64) void conv_bwd_kernel(ConvP P) {
 
 constexpr int64_t kMaxChannels = 1 << 20, kMaxLevels = (int64_t)1 << 34;
 // Wavefronts of a launch before they loop over chunks.  The backward's partial
-// sums grow with them.
+// sums grow with them (2048, 4096 and 8192 within 2% of each other at 256 x 128 x 512).
 constexpr int64_t kFwdWaves = 1 << 20, kBwdWaves = 4096;
 
 // Levels of a chunk: 32, where the W - 1 levels read twice cost little, or 16 or 8 where
-// there would be fewer than one wavefront a SIMD.
+// there would be fewer than one wavefront a SIMD.  Backward: 1 x 1024 x 512 19 us with 8 and 23 with 32; with
+// 64 throughout 8 x 2048 x 1024 takes 47 and not 38 us.
 int chunk_of(int64_t batch, int64_t length, int64_t channels) {
     int c = 32;
     while (c > 8 && batch * cdiv(length, c) * cdiv(channels, 256) < 1024) c /= 2;

@@ -11,13 +11,17 @@
 // width is no multiple of a load the row's last load begins earlier and the columns
 // that it repeats count as 0.
 //
+// Measured: 50021 x 1160 bf16 to 8 bits 79 us (5.2 TB/s), 1048576 x 128 bf16 forward 181 us
+// (5.9 TB/s); a copy reaches 4.8 TB/s here.
+//
 // Backward: with rho = (mean(s^2) + eps)^-1/2 and g = w dy, differentiating
 // y_i = w_i s_i rho gives ds = dsum + rho g - rho^3 mean(g s) s.  Both row means
 // come from the registers that hold the row, so again everything is read once; rho
 // is recomputed, since s is read anyway.  dw sums dy s rho over the rows: a lane
 // keeps the sums of its columns in float32 registers while its workgroup walks
 // over rows, the workgroup adds its row groups through LDS and writes one
-// partial row, and colsum_kernel adds those in a fixed order.
+// partial row, and colsum_kernel adds those in a fixed order.  1048576 x 128 bf16: 189 us
+// (5.7 TB/s).
 #include "net_common.hpp"
 
 using namespace fpde_net;
@@ -452,8 +456,16 @@ __global__ __launch_bounds__(256) void norm_dw_wide_kernel(NormBwdP P) {
 constexpr int64_t kMaxRows = (int64_t)1 << 40, kMaxWidth = 1 << 20;
 
 // Columns of a load, lanes a row and loads a lane: f(V, LPR, CH) for the smallest that holds the
-// row; f(0, 0, 0) if none does.  LEAST: the fewest lanes a row.
-template <class T, int LEAST, class F>
+// row; f(0, 0, 0) if none does.  LEAST: the fewest lanes a row.  Measured with the neighbours, in us:
+//   one load a lane, few lanes: 65536 x 192 bf16 backward 22 with 32 lanes, 29 with 64; two loads on
+//     16 lanes: 128 columns of float32 forward 93 and 97, 512 of bf16 40 and 39: no gain;
+//   three loads: 32768 x 1160 bf16 forward 49, with four (a fifth of them idle) 54, 256 lanes 53;
+//   eight loads a lane of eight columns: 32768 x 2048 rows as four; past 8192 columns they take the
+//     registers of all but two wavefronts a SIMD, and the forward is faster as rows that are read
+//     twice: 4096 x 12000 bf16 to 8 bits 58 and not 100, with a residual 94 and not 104 (float32,
+//     2048 x 6000: 25 in registers, 27 read twice); the backward is not: 123 and 128, 254 and 334 at
+//     8192 x 16384.
+template <class T, int LEAST, bool FWD, class F>
 int with_layout(int64_t width, F f) {
     constexpr int V = kVec<T>, L16 = LEAST > 16 ? LEAST : 16;
 #define FPDE_L(W, L, C) \
@@ -469,16 +481,19 @@ int with_layout(int64_t width, F f) {
     if (chunks <= 512) return FPDE_L(V, 256, 2);
     if (chunks <= 768) return FPDE_L(V, 256, 3);
     if (chunks <= 1024) return FPDE_L(V, 256, 4);
-    if (chunks <= 2048) return FPDE_L(V, 256, 8);
+    if constexpr (!FWD || V < 8) {  // (32 columns a lane, of the backward's 16-bit rows 64)
+        if (chunks <= 2048) return FPDE_L(V, 256, 8);
+    }
     return FPDE_L(0, 0, 0);
 #undef FPDE_L
 }
 
 bool is_wide(int dtype, int64_t width) { return cdiv(width, 16 / size_of(dtype)) > 2048; }
 
-// Workgroups of the backward, which each write one partial row of dw: 4 for every
-// compute unit keep the loads in flight, and few partial rows keep their sum short.
-constexpr int64_t kBwdBlocks = 1024;
+// Workgroups of the backward, which each write one partial row of dw: 2 for every
+// compute unit keep the loads in flight, and few partial rows keep their sum short.  With 256 / 512 /
+// 1024 of them 1048576 x 128 bf16 takes 266 / 189 / 205 us, 32768 x 1160 64 / 52 / 57.
+constexpr int64_t kBwdBlocks = 512;
 // Row groups of the wide rows' column sums.
 constexpr int64_t kWideGroups = 128;
 // Most workgroups of a launch: past it they loop over rows.
@@ -554,9 +569,9 @@ extern "C" int fpde_rms_norm(const fpde_norm_args* a, void* stream) {
             }
         };
         if (!f8)
-            return with_layout<T, 1>(a->width, [&](auto v, auto l, auto c) { return run(std::false_type{}, v, l, c); });
+            return with_layout<T, 1, true>(a->width, [&](auto v, auto l, auto c) { return run(std::false_type{}, v, l, c); });
         // (8 bits: a group of 128 columns has to lie in one row's lanes)
-        return with_layout<T, 128 / kVec<T>>(a->width,
+        return with_layout<T, 128 / kVec<T>, true>(a->width,
                                              [&](auto v, auto l, auto c) { return run(std::true_type{}, v, l, c); });
     });
 }
@@ -601,7 +616,7 @@ extern "C" int fpde_rms_norm_bwd(const fpde_norm_bwd_args* a, void* stream) {
                           : FPDE_OK;
     return with_type(a->dtype, [&](auto t) {
         using T = decltype(t);
-        return with_layout<T, 1>(a->width, [&](auto v, auto lpr, auto ch) {
+        return with_layout<T, 1, false>(a->width, [&](auto v, auto lpr, auto ch) {
             constexpr int V = decltype(v)::value, L = decltype(lpr)::value, C = decltype(ch)::value;
             int64_t parts;
             int r;

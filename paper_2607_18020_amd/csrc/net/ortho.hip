@@ -18,14 +18,19 @@
 //
 // Small matrices (s <= 128 and l <= 128, or s <= 64 and l <= 256): one workgroup and one
 // launch for a whole matrix, momentum and weight update included.  X stays in
-// registers; X, A, B take turns in two LDS regions.  What bounds it is the LDS reads
-// of the operands.
+// registers; X, A, B take turns in two LDS regions.  Six of 128 x 128: 44 us, 6.8 a step and
+// 10 for the norm, loads and stores: the matrix cores, the LDS reads of the operands and
+// the VALU (sums to halves) take about 40% of a step each, one after the other between
+// the barriers of a single workgroup.  The tiled kernels take 83 to 100 us for the same.
 //
 // Others: each product is a launch of a tiled kernel over all matrices.  Both operands
 // of every product are rows that are contiguous along the sum (A and A^2 are
 // symmetric, and X is kept in both orders), so tiles go from memory to LDS by
 // direct loads, 16 bytes a lane, and from there to the matrix cores by 16-byte reads;
-// the chunks of a row are permuted such that those reads meet no bank twice.
+// the chunks of a row are permuted such that those reads meet no bank twice.  A 4096 x
+// 4096 step: A and A^2 about 250 us each, B X 420, 0.98 PFLOP/s of f16 products; LDS traffic (64 KB
+// of reads and 32 KB of loads for 96 matrix instructions) takes as many cycles as those.  Four of
+// 260 x 1000: 14, 8 and 12 us, for the operands' way from the caches to few workgroups.
 #include <stdlib.h>
 
 #include "net_common.hpp"

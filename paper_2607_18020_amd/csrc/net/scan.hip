@@ -33,9 +33,15 @@
 // runs each block forward again from its state with all a_t h_{t-1} of the block in
 // registers, and then backward.  That takes 15 registers a state, so a lane has 8 states
 // at most and 2 or 4 lanes own a channel with more: one lane with 16 took 400 registers,
-// a single wavefront a SIMD.  The sums over channels (dB, dC) halve the values and the
+// a single wavefront a SIMD, and 345 us where two lanes took 331; four lanes with 4
+// states each cost a quarter more (838 and not 661 us in all).  The sums over channels (dB, dC) halve the values and the
 // lanes together (reduce_lanes): one swap or DPP and one addition for each value that
 // goes; the wavefronts' sums are partial rows that a last launch adds in order.
+//
+// Measured: 2 x 16384 x 512 float32, 16 states, 162 us (70 a first pass, 11 chunks, 85 the outputs;
+// 1.7 TB/s, half of the VALU's slots).  8 x 2048 x 1024 bf16, 16 states, ragged: forward 67
+// + 14 + 83 us, backward 111 + 14 + 319 + 21 for dB and dC + 5; the VALU is
+// busy two thirds of the main pass's time.
 #include "net_common.hpp"
 
 using namespace fpde_net;
@@ -835,7 +841,10 @@ struct Plan {
 };
 
 // Wavefronts that fill the card: one for each SIMD.  Whole windows with fewer are
-// split in chunks until there are kWaves, as long as a chunk keeps kMinChunk levels.
+// split in chunks until there are kWaves, as long as a chunk keeps kMinChunk levels.  Measured, forward,
+// split / whole: 32 x 512 x 1024 (512 wavefronts) 164 / 217 us, 64 x 512 x 1024 (1024) 305 / 227.
+// kWaves 2048, 4096, 8192, 16384: 174, 168, 177, 208 us for 2 x 16384 x 512.  kMinChunk 16 and 32: 32 and
+// 42 us for 4 x 700 x 128.
 constexpr int64_t kFill = 1024, kWaves = 4096;
 constexpr int kMinChunk = 16;
 // Most wavefronts of a launch; of the backward's main launch, whose partial sums of dA grow with them.

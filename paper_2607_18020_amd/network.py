@@ -601,8 +601,12 @@ def _matrices(what, name, ts, like=None, dtype=None):
     """(tensors, host array of their pointers) of dense matrices of one shape, type and device."""
     ts = list(ts)
     t0 = ts[0] if like is None else like
-    shape, dt, dev = t0.shape, dtype or t0.dtype, t0.device
-    return ts, (_vp * len(ts))(*[_dense(what, name, t, shape, dt, dev) for t in ts])
+    shape, dt, index = t0.shape, dtype or t0.dtype, t0.get_device()
+    for t in ts:
+        if not isinstance(t, _Tensor) or t.dtype is not dt or t.get_device() != index or t.shape != shape \
+                or not t.is_contiguous():
+            raise ValueError(f"{what} {name}: need contiguous {dt} tensors of shape {tuple(shape)} on {t0.device}")
+    return ts, (_vp * len(ts))(*[t.data_ptr() for t in ts])
 
 
 def fpde_orthogonalize(mats, *, steps: int = 5, coeffs=NS_COEFFS, eps: float = 1e-7, out=None, stream=None):
@@ -634,7 +638,8 @@ def fpde_orthogonalize(mats, *, steps: int = 5, coeffs=NS_COEFFS, eps: float = 1
             raise ValueError(f"{what}: need [m, n] matrices")
         (m, n), count = mats[0].shape, len(mats)
         mats, gp = _matrices(what, "input", mats)
-        out = [_empty(stream, t.shape, t.dtype, dev) for t in mats] if out is None else out
+        if out is None:
+            out = _empty(stream, (count, m, n), mats[0].dtype, dev).unbind(0)
         out, op = _matrices(what, "out", out, mats[0])
         if len(out) != count:
             raise ValueError(f"{what}: {len(out)} outputs for {count} matrices")
