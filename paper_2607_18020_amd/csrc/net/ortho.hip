@@ -30,7 +30,7 @@
 // the chunks of a row are permuted such that those reads meet no bank twice.  A 4096 x
 // 4096 step: A and A^2 about 250 us each, B X 420, 0.98 PFLOP/s of f16 products; LDS traffic (64 KB
 // of reads and 32 KB of loads for 96 matrix instructions) takes as many cycles as those.  Four of
-// 260 x 1000: 14, 8 and 12 us, for the operands' way from the caches to few workgroups.
+// 260 x 1000: 10, 7 and 12 us, for the operands' way from the caches to few workgroups.
 #include <stdlib.h>
 
 #include "net_common.hpp"
@@ -626,6 +626,80 @@ __global__ __launch_bounds__(256 * KG) void ortho_product_kernel(Prod P, Mats M)
     }
 }
 
+// The same for a few small matrices, where a launch takes as long as its operands need to come: tiles of
+// 32, and 16 wavefronts that each have a 16th of the sum's length, straight from memory to registers.
+// All loads of 16 U k are in flight at once, and no wavefront waits for another before the sums meet.
+template <int U, bool LAST, class T>
+__global__ __launch_bounds__(1024) void ortho_product32_kernel(Prod P, Mats M) {
+    constexpr int WAVES = 16, PT = 33;
+    __shared__ float part[WAVES][32][32];
+    __shared__ float tile[32][PT];
+    const int lane = (int)(threadIdx.x & 63), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int all = (int)gridDim.x, whole = all & ~7, id = (int)blockIdx.x;
+    const int at = id < whole ? (id & 7) * (whole >> 3) + (id >> 3) : id;
+    const int mat = at / P.tiles;
+    int tr, tc;
+    tile_at(at - mat * P.tiles, P.tm, P.tn, P.sym, &tr, &tc);
+    const int r = lane & 31, kh = lane >> 5, row = (int)threadIdx.x >> 5, col = (int)threadIdx.x & 31;
+    float z = 0.f;
+    if (P.Z.hi) {
+        const int64_t i = mat * P.Z.step + (int64_t)(tr * 32 + row) * P.Z.ld + tc * 32 + col;
+        z = (float)P.Z.hi[i] + (float)P.Z.lo[i];
+    }
+    const int64_t iu = mat * P.U.step + (int64_t)(tr * 32 + r) * P.U.ld + kh * 8;
+    const int64_t iv = mat * P.V.step + (int64_t)(tc * 32 + r) * P.V.ld + kh * 8;
+    const int chunks = P.K / 16, per = (chunks + WAVES - 1) / WAVES, c0 = wave * per;
+    const int c1 = c0 + per < chunks ? c0 + per : chunks;
+    f32x16 acc[2];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[0][e] = acc[1][e] = 0.f;
+    for (int c = c0; c < c1; c += U) {
+        f16x8 uh[U], ul[U], vh[U], vl[U];
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            const int k = (c + j < c1 ? c + j : c1 - 1) * 16;
+            uh[j] = *(const f16x8*)(P.U.hi + iu + k);
+            vh[j] = *(const f16x8*)(P.V.hi + iv + k);
+            ul[j] = *(const f16x8*)(P.U.lo + iu + k);
+            vl[j] = *(const f16x8*)(P.V.lo + iv + k);
+        }
+#pragma unroll
+        for (int j = 0; j < U; ++j)
+            if (c + j < c1) {
+                acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(uh[j], vl[j], acc[0], 0, 0, 0);
+                acc[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(uh[j], vh[j], acc[1], 0, 0, 0);
+                acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ul[j], vh[j], acc[0], 0, 0, 0);
+            }
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) part[wave][(e & 3) + 8 * (e >> 2) + 4 * kh][r] = acc[0][e] + acc[1][e];
+    __syncthreads();
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) v += part[w][row][col];
+    tile[row][col] = fmaf(P.ca, z, v * P.cp);
+    __syncthreads();
+    // two wavefronts an order, 8 elements a lane
+    const int q = (int)threadIdx.x & 127, i = q >> 2, j = (q & 3) * 8;
+    if (threadIdx.x >= 256 || (LAST && (threadIdx.x >= 128) != (M.tall != 0))) return;
+    float o[8];
+    const bool turned = threadIdx.x >= 128;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = turned ? tile[j + e][i] : tile[i][j + e];
+    const int grow = (turned ? tc : tr) * 32 + i, gcol = (turned ? tr : tc) * 32 + j;
+    if constexpr (LAST) {
+        if (grow < M.m && gcol < M.n) finish<T>(M, mat, (int64_t)grow * M.n + gcol, o, M.n - gcol);
+    } else {
+        if (turned && P.sym && tr == tc) return;
+        const Half& H = turned ? P.Ct : P.C;
+        f16x8 hi, lo;
+        split<8>(o, hi, lo);
+        const int64_t c = mat * H.step + (int64_t)grow * H.ld + gcol;
+        *(f16x8*)(H.hi + c) = hi;
+        *(f16x8*)(H.lo + c) = lo;
+    }
+}
+
 // ---------------------------------------------------------------------------
 // Host side.
 
@@ -700,8 +774,26 @@ int run_large(const Mats& M, const OrthoPlan& p, int count, int steps, float ca,
                    M, part, X[0], Xt[0]);
     const int ts = (int)(p.sp / p.tile), tl = (int)(p.lp / p.tile), tri = ts * (ts + 1) / 2;
     auto product = [&](Prod P, bool last) {
-        dim3 g((unsigned)(P.tiles * count));
+        const int64_t t32 = p.sp / 32, n32 = (P.sym ? t32 * (t32 + 1) / 2 : t32 * (p.lp / 32)) * count;
         P.first = P.quarters = 0;
+        // Up to one workgroup for every compute unit of tiles of 32.  Five steps with these / tiles of 64:
+        // one 256 x 256 matrix 98 / 118 us, one 512 x 512 134 / 155, four of 260 x 1000 (the symmetric ones) 162 / 178;
+        // with up to 512 of them eight of 256 x 256 (288) take 238 and not 122.
+        if (p.tile == 64 && n32 <= kUnits) {
+            P.tm = (int)t32, P.tn = P.sym ? (int)t32 : (int)(p.lp / 32), P.tiles = (int)(n32 / count);
+            const dim3 g((unsigned)n32);
+            // (no more loads a lane than its share of the sum has: with four times 16 k for all, a 256 x 256
+            // matrix takes 142 us)
+            auto direct = [&](auto u) {
+                constexpr int U = decltype(u)::value;
+                return last ? launch(ortho_product32_kernel<U, true, T>, g, dim3(1024), s, P, M)
+                            : launch(ortho_product32_kernel<U, false, float>, g, dim3(1024), s, P, M);
+            };
+            return P.K <= 256   ? direct(std::integral_constant<int, 1>{})
+                   : P.K <= 512 ? direct(std::integral_constant<int, 2>{})
+                                : direct(std::integral_constant<int, 4>{});
+        }
+        dim3 g((unsigned)(P.tiles * count));
         if (p.tile == 128) {
             // The last few tiles past a multiple of the compute units would be a round that few of them
             // share: their quarters go to as many, in a launch of their own.  Five steps with / without:

@@ -202,3 +202,13 @@ def test_quarters_of_the_last_tiles(N, count, m, n):
         r = R.orthogonalize(g[i].cuda().double(), 3, CO, 1e-7).cpu()
         near("orthogonalize", o[i], r)
         near("weight", wc[i], w[i].double() - 0.05 * max(1.0, m / n) ** 0.5 * r)
+
+
+@pytest.mark.parametrize("count,m,n", [(2, 530, 700), (1, 1100, 1090), (1, 1500, 1510), (3, 300, 310), (1, 250, 770)])
+def test_tiles_of_32_and_64(N, count, m, n):
+    """Between the tiles of 32 and those of 128, and a sum shared by wavefronts or not."""
+    print(f"case ortho {count} of {m} x {n}", flush=True)
+    g = torch.stack([matrix(m, n, s) for s in range(count)]).cuda()
+    o = N.fpde_orthogonalize(g, steps=4)
+    for i in range(count):
+        near("orthogonalize", o[i], R.orthogonalize(g[i].double(), 4, CO, 1e-7).cpu())
