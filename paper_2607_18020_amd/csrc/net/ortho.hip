@@ -24,10 +24,10 @@
 // the barriers of a single workgroup.  The tiled kernels take 83 to 100 us for the same.
 //
 // Others: each product is a launch of a tiled kernel over all matrices.  Both operands
-// of every product are rows that are contiguous along the sum (A and A^2 are
+// of every product are rows of 16-byte chunks along the sum (A and A^2 are
 // symmetric, and X is kept in both orders), so tiles go from memory to LDS by
 // direct loads, 16 bytes a lane, and from there to the matrix cores by 16-byte reads;
-// the chunks of a row are permuted such that those reads meet no bank twice.  A 4096 x
+// neighbouring rows' chunks follow each other in both, so those reads meet no bank twice.  A 4096 x
 // 4096 step: A and A^2 about 250 us each, B X 420, 0.98 PFLOP/s of f16 products; LDS traffic (64 KB
 // of reads and 32 KB of loads for 96 matrix instructions) takes as many cycles as those.  Four of
 // 260 x 1000: 10, 7 and 12 us, for the operands' way from the caches to few workgroups.
@@ -350,20 +350,25 @@ __global__ __launch_bounds__(256) void ortho_norm_kernel(Mats M, double* part) {
     if (threadIdx.x == 0) part[mat * kNormBlocks + blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
 }
 
-// Halves of one [rows][cols] matrix of all matrices of a launch, `step` elements apart.
+// Halves of one matrix of all matrices of a launch, `step` elements apart.  Eight neighbouring columns of a
+// row are 16 bytes, those of the next row follow, and the next eight columns come after all `rows`: what a
+// wavefront reads or writes, 8 columns of rows in turn, is one stretch of memory.
 struct Half {
     f16 *hi, *lo;
     int64_t step;
-    int ld;
+    int rows;
+    __device__ __forceinline__ int64_t at(int mat, int row, int col) const {
+        return mat * step + ((int64_t)(col >> 3) * rows + row) * 8 + (col & 7);
+    }
+    // 8 columns of a row
+    __device__ __forceinline__ void put(int mat, int row, int col, const float (&v)[8]) const {
+        f16x8 h, l;
+        split<8>(v, h, l);
+        const int64_t i = at(mat, row, col);
+        *(f16x8*)(hi + i) = h;
+        *(f16x8*)(lo + i) = l;
+    }
 };
-
-// two neighbouring values of a row
-__device__ __forceinline__ void put_halves(float a, float b, const Half& H, int64_t i) {
-    f16x2 hi, lo;
-    split2(a * kS, b * kS, hi, lo);
-    *(f16x2*)(H.hi + i) = hi;
-    *(f16x2*)(H.lo + i) = lo;
-}
 
 // X0 in both orders, zeros in the padding.  64 x 64 tiles of X; 256 threads.
 template <class T>
@@ -397,13 +402,15 @@ __global__ __launch_bounds__(256) void ortho_split_kernel(Mats M, const double* 
         (M.tall ? tile[lane][i] : tile[i][lane]) = in ? inv * update_of(M, g[h], m[h]) : 0.f;
     });
     __syncthreads();
-    // two columns a lane, two rows a wavefront
-    const int i0 = wave * 2 + (lane >> 5), j = (lane & 31) * 2;
+    // a lane a row, eight of its columns at a time
 #pragma unroll
-    for (int h = 0; h < 8; ++h) {
-        const int i = i0 + h * 8;
-        put_halves(tile[i][j], tile[i][j + 1], X, mat * X.step + (int64_t)(r0 + i) * X.ld + c0 + j);
-        put_halves(tile[j][i], tile[j + 1][i], Xt, mat * Xt.step + (int64_t)(c0 + i) * Xt.ld + r0 + j);
+    for (int h = 0; h < 2; ++h) {
+        const int j = (wave * 2 + h) * 8;
+        float v[8], vt[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = tile[lane][j + e] * kS, vt[e] = tile[j + e][lane] * kS;
+        X.put(mat, r0 + lane, c0 + j, v);
+        Xt.put(mat, c0 + lane, r0 + j, vt);
     }
 }
 
@@ -471,26 +478,24 @@ __global__ __launch_bounds__(256 * KG) void ortho_product_kernel(Prod P, Mats M)
         tr = tr * 2 + (own >> 1 & 1), tc = tc * 2 + (own & 1);
         if (P.sym && tr > tc) return;
     }
-    const f16* src[4] = {P.U.hi + mat * P.U.step + (int64_t)tr * TILE * P.U.ld,
-                         P.U.lo + mat * P.U.step + (int64_t)tr * TILE * P.U.ld,
-                         P.V.hi + mat * P.V.step + (int64_t)tc * TILE * P.V.ld,
-                         P.V.lo + mat * P.V.step + (int64_t)tc * TILE * P.V.ld};
-    // Chunk q of a tile holds row q / 4; of the row's four chunks of 8 k it is number (q % 4) ^ (row / 4 % 4),
-    // so that 16 rows' chunks of one k lie in different banks.
+    const int64_t iu = P.U.at(mat, tr * TILE, 0), iv = P.V.at(mat, tc * TILE, 0);
+    const f16* src[4] = {P.U.hi + iu, P.U.lo + iu, P.V.hi + iv, P.V.lo + iv};
+    // Chunk q of a tile holds 8 k of row q % TILE: q / TILE, of four.  Neighbouring rows' chunks of one k
+    // lie in different banks.
     auto fetch = [&](int k, int buf) {
 #pragma unroll
         for (int o = 0; o < 4; ++o)
 #pragma unroll
             for (int i = 0; i < CH / 256; ++i) {
-                const int q0 = i * 256 + wave * 64, q = q0 + lane, row = q >> 2, ch = (q & 3) ^ ((row >> 2) & 3);
-                const f16* g = src[o] + (int64_t)row * (o < 2 ? P.U.ld : P.V.ld) + k + ch * 8;
+                const int q0 = i * 256 + wave * 64, q = q0 + lane, row = q % TILE, ch = q / TILE;
+                const f16* g = src[o] + ((int64_t)(k / 8 + ch) * (o < 2 ? P.U.rows : P.V.rows) + row) * 8;
                 __builtin_amdgcn_global_load_lds((gptr_t)g, (lptr_t)(lds + (((kg * NB + buf) * 4 + o) * CH + q0) * 16), 16, 0,
                                                  0);
             }
     };
     const int wr = (wave >> 1) * W, wc = (wave & 1) * W, r = lane & 31, kh = lane >> 5;
     auto operand = [&](int o, int buf, int row, int ch) {
-        return *(const f16x8*)(lds + (((kg * NB + buf) * 4 + o) * CH + row * 4 + (ch ^ ((row >> 2) & 3))) * 16);
+        return *(const f16x8*)(lds + (((kg * NB + buf) * 4 + o) * CH + ch * TILE + row) * 16);
     };
     // A sum's three products in turn would each wait for the one before: with four tiles a wavefront
     // they are four instructions apart, with one tile each has a sum of its own.
@@ -548,14 +553,14 @@ __global__ __launch_bounds__(256 * KG) void ortho_product_kernel(Prod P, Mats M)
     f16x8 zh[IT], zl[IT];
     auto place = [&](int it, int* row, int* col) {
         const int q = it * THREADS + (writer ? (int)threadIdx.x : 0);
-        *row = q / (TILE / 8), *col = q % (TILE / 8) * 8;
+        *row = q % TILE, *col = q / TILE * 8;
     };
     if (P.Z.hi) {
 #pragma unroll
         for (int it = 0; it < IT; ++it) {
             int row, col;
             place(it, &row, &col);
-            const int64_t z = mat * P.Z.step + (int64_t)(tr * TILE + row) * P.Z.ld + tc * TILE + col;
+            const int64_t z = P.Z.at(mat, tr * TILE + row, tc * TILE + col);
             zh[it] = *(const f16x8*)(P.Z.hi + z);
             zl[it] = *(const f16x8*)(P.Z.lo + z);
         }
@@ -574,14 +579,7 @@ __global__ __launch_bounds__(256 * KG) void ortho_product_kernel(Prod P, Mats M)
                 t[(wr + i * 32 + (e & 3) + 8 * (e >> 2) + 4 * kh) * PT + wc + j * 32 + r] = v * P.cp;
             }
     __syncthreads();
-    auto put = [&](const Half& H, int row, int col, const float (&v)[8]) {
-        f16x8 hi, lo;
-        split<8>(v, hi, lo);
-        const int64_t c = mat * H.step + (int64_t)row * H.ld + col;
-        *(f16x8*)(H.hi + c) = hi;
-        *(f16x8*)(H.lo + c) = lo;
-    };
-    const bool both = LAST ? M.tall : !(P.sym && tr == tc);
+    const bool both = LAST || !(P.sym && tr == tc);
     t = tile;
 #pragma unroll
     for (int it = 0; it < IT; ++it) {
@@ -600,28 +598,33 @@ __global__ __launch_bounds__(256 * KG) void ortho_product_kernel(Prod P, Mats M)
 #pragma unroll
             for (int e = 0; e < 8; ++e) t[row * PT + col + e] = v[e];
         }
-        const int grow = tr * TILE + row, gcol = tc * TILE + col;
-        if constexpr (LAST) {
-            if (!M.tall && grow < M.m && gcol < M.n) finish<T>(M, mat, (int64_t)grow * M.n + gcol, v, M.n - gcol);
-        } else {
-            put(P.C, grow, gcol, v);
-        }
+        if constexpr (!LAST) P.C.put(mat, tr * TILE + row, tc * TILE + col, v);
     }
     if (!both) return;
     __syncthreads();
 #pragma unroll
     for (int it = 0; it < IT; ++it) {
         if (!writer) break;
-        // 16 neighbouring columns and 4 groups of rows a wavefront: few lanes meet in a bank
-        const int q = it * THREADS + (int)threadIdx.x, col = q % 16 + q / (16 * (TILE / 8)) * 16;
-        const int row = q / 16 % (TILE / 8) * 8, grow = tr * TILE + row, gcol = tc * TILE + col;
+        const int q = it * THREADS + (int)threadIdx.x;
         float v[8];
+        if constexpr (!LAST) {
+            const int col = q % TILE, row = q / TILE * 8;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = t[(row + e) * PT + col];
-        if constexpr (LAST) {
+            for (int e = 0; e < 8; ++e) v[e] = t[(row + e) * PT + col];
+            P.Ct.put(mat, tc * TILE + col, tr * TILE + row, v);
+        } else if (M.tall) {
+            // 16 neighbouring columns and 4 groups of rows a wavefront: few lanes meet in a bank
+            const int col = q % 16 + q / (16 * (TILE / 8)) * 16, row = q / 16 % (TILE / 8) * 8;
+            const int grow = tr * TILE + row, gcol = tc * TILE + col;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = t[(row + e) * PT + col];
             if (gcol < M.m && grow < M.n) finish<T>(M, mat, (int64_t)gcol * M.n + grow, v, M.n - grow);
         } else {
-            put(P.Ct, gcol, grow, v);
+            const int row = q / (TILE / 8), col = q % (TILE / 8) * 8;
+            const int grow = tr * TILE + row, gcol = tc * TILE + col;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = t[row * PT + col + e];
+            if (grow < M.m && gcol < M.n) finish<T>(M, mat, (int64_t)grow * M.n + gcol, v, M.n - gcol);
         }
     }
 }
@@ -643,11 +646,9 @@ __global__ __launch_bounds__(1024) void ortho_product32_kernel(Prod P, Mats M) {
     const int r = lane & 31, kh = lane >> 5, row = (int)threadIdx.x >> 5, col = (int)threadIdx.x & 31;
     float z = 0.f;
     if (P.Z.hi) {
-        const int64_t i = mat * P.Z.step + (int64_t)(tr * 32 + row) * P.Z.ld + tc * 32 + col;
+        const int64_t i = P.Z.at(mat, tr * 32 + row, tc * 32 + col);
         z = (float)P.Z.hi[i] + (float)P.Z.lo[i];
     }
-    const int64_t iu = mat * P.U.step + (int64_t)(tr * 32 + r) * P.U.ld + kh * 8;
-    const int64_t iv = mat * P.V.step + (int64_t)(tc * 32 + r) * P.V.ld + kh * 8;
     const int chunks = P.K / 16, per = (chunks + WAVES - 1) / WAVES, c0 = wave * per;
     const int c1 = c0 + per < chunks ? c0 + per : chunks;
     f32x16 acc[2];
@@ -657,11 +658,12 @@ __global__ __launch_bounds__(1024) void ortho_product32_kernel(Prod P, Mats M) {
         f16x8 uh[U], ul[U], vh[U], vl[U];
 #pragma unroll
         for (int j = 0; j < U; ++j) {
-            const int k = (c + j < c1 ? c + j : c1 - 1) * 16;
-            uh[j] = *(const f16x8*)(P.U.hi + iu + k);
-            vh[j] = *(const f16x8*)(P.V.hi + iv + k);
-            ul[j] = *(const f16x8*)(P.U.lo + iu + k);
-            vl[j] = *(const f16x8*)(P.V.lo + iv + k);
+            const int k = (c + j < c1 ? c + j : c1 - 1) * 16 + kh * 8;
+            const int64_t iu = P.U.at(mat, tr * 32 + r, k), iv = P.V.at(mat, tc * 32 + r, k);
+            uh[j] = *(const f16x8*)(P.U.hi + iu);
+            vh[j] = *(const f16x8*)(P.V.hi + iv);
+            ul[j] = *(const f16x8*)(P.U.lo + iu);
+            vl[j] = *(const f16x8*)(P.V.lo + iv);
         }
 #pragma unroll
         for (int j = 0; j < U; ++j)
@@ -680,7 +682,7 @@ __global__ __launch_bounds__(1024) void ortho_product32_kernel(Prod P, Mats M) {
     tile[row][col] = fmaf(P.ca, z, v * P.cp);
     __syncthreads();
     // two wavefronts an order, 8 elements a lane
-    const int q = (int)threadIdx.x & 127, i = q >> 2, j = (q & 3) * 8;
+    const int q = (int)threadIdx.x & 127, i = LAST ? q >> 2 : q & 31, j = (LAST ? q & 3 : q >> 5) * 8;
     if (threadIdx.x >= 256 || (LAST && (threadIdx.x >= 128) != (M.tall != 0))) return;
     float o[8];
     const bool turned = threadIdx.x >= 128;
@@ -691,12 +693,7 @@ __global__ __launch_bounds__(1024) void ortho_product32_kernel(Prod P, Mats M) {
         if (grow < M.m && gcol < M.n) finish<T>(M, mat, (int64_t)grow * M.n + gcol, o, M.n - gcol);
     } else {
         if (turned && P.sym && tr == tc) return;
-        const Half& H = turned ? P.Ct : P.C;
-        f16x8 hi, lo;
-        split<8>(o, hi, lo);
-        const int64_t c = mat * H.step + (int64_t)grow * H.ld + gcol;
-        *(f16x8*)(H.hi + c) = hi;
-        *(f16x8*)(H.lo + c) = lo;
+        (turned ? P.Ct : P.C).put(mat, grow, gcol, o);
     }
 }
 
@@ -760,7 +757,7 @@ int run_large(const Mats& M, const OrthoPlan& p, int count, int steps, float ca,
     at += p.batch * kNormBlocks * (int64_t)sizeof(double);
     auto half = [&](int64_t rows, int64_t cols) {
         Half h;
-        h.hi = (f16*)at, h.step = rows * cols, h.ld = (int)cols;
+        h.hi = (f16*)at, h.step = rows * cols, h.rows = (int)rows;
         h.lo = h.hi + p.batch * rows * cols;
         at += p.batch * rows * cols * 4;
         return h;
