@@ -21,16 +21,18 @@
 // registers; X, A, B take turns in two LDS regions.  Six of 128 x 128: 44 us, 6.8 a step and
 // 10 for the norm, loads and stores: the matrix cores, the LDS reads of the operands and
 // the VALU (sums to halves) take about 40% of a step each, one after the other between
-// the barriers of a single workgroup.  The tiled kernels take 83 to 100 us for the same.
+// the barriers of a single workgroup.  The tiled kernels, a launch a product, take twice as long.
 //
 // Others: each product is a launch of a tiled kernel over all matrices.  Both operands
 // of every product are rows of 16-byte chunks along the sum (A and A^2 are
 // symmetric, and X is kept in both orders), so tiles go from memory to LDS by
 // direct loads, 16 bytes a lane, and from there to the matrix cores by 16-byte reads;
 // neighbouring rows' chunks follow each other in both, so those reads meet no bank twice.  A 4096 x
-// 4096 step: A and A^2 about 250 us each, B X 420, 0.98 PFLOP/s of f16 products; LDS traffic (64 KB
-// of reads and 32 KB of loads for 96 matrix instructions) takes as many cycles as those.  Four of
-// 260 x 1000: 10, 7 and 12 us, for the operands' way from the caches to few workgroups.
+// 4096 step: A and A^2 186 + 35 us each, B X 370 to 420 with the card's clock, 1.0 to 1.1 PFLOP/s of
+// f16 products, where a library's plain f16 product reaches 1.19; LDS traffic (64 KB of reads and
+// 32 KB of loads for 96 matrix instructions) takes as many cycles as those.  Four of 260 x
+// 1000: 8, 6 and 11 us, a 512 x 512 matrix 6 to 7 each: what a launch, one trip to the caches of the other
+// XCDs for the operands and one back take.
 #include <stdlib.h>
 
 #include "net_common.hpp"
@@ -723,8 +725,9 @@ OrthoPlan plan(int64_t count, int64_t m, int64_t n) {
     p.batch = kMaxCount, p.bytes = 0, p.tile = 0, p.sp = p.lp = 0;
     if (p.small) return p;
     // Tiles of 128 need half the reads of 64 a flop, but only where they are enough for half of the
-    // compute units.  Five steps, tiles of 128 / 64: one 2048 x 2048 matrix (136 tiles) 945 / 980 us, two of
-    // 1536 x 1536 (156) 880 / 860 us, one of 2560 x 2560 (210) 1480 / 1950 us, one of 1536 x 1536 (78) 732 / 523 us.
+    // compute units.  Five steps, tiles of 128 / 64: one 1700 x 1700 matrix (105 tiles) 712 / 549 us, one of
+    // 2048 x 2048 (136) 830 / 833, one of 2304 x 2304 (171) 1087 / 1097, one of 2560 x 2560 (210) 1480 / 1950
+    // (before the operands' layout became what it is).
     const int64_t t = cdiv(p.s, 128);
     p.tile = t * (t + 1) / 2 * (count < 1 ? 1 : count) >= kUnits / 2 ? 128 : 64;
     p.sp = cdiv(p.s, p.tile) * p.tile, p.lp = cdiv(p.l, p.tile) * p.tile;
@@ -773,14 +776,14 @@ int run_large(const Mats& M, const OrthoPlan& p, int count, int steps, float ca,
     auto product = [&](Prod P, bool last) {
         const int64_t t32 = p.sp / 32, n32 = (P.sym ? t32 * (t32 + 1) / 2 : t32 * (p.lp / 32)) * count;
         P.first = P.quarters = 0;
-        // Up to one workgroup for every compute unit of tiles of 32.  Five steps with these / tiles of 64:
-        // one 256 x 256 matrix 98 / 118 us, one 512 x 512 134 / 155, four of 260 x 1000 (the symmetric ones) 162 / 178;
-        // with up to 512 of them eight of 256 x 256 (288) take 238 and not 122.
-        if (p.tile == 64 && n32 <= kUnits) {
+        // Tiles of 32, up to two workgroups of them for every compute unit.  Five steps with these / with tiles
+        // of 64: two 512 x 512 matrices (272 for a symmetric product, 512) 126 / 152 us, eight of 256 x 256 (288, 512)
+        // 102 / 118; with more, 235 / 211 for 1024 x 1024 (528, 1024), 150 / 142 for three of 512 x 512 (408, 768).
+        if (p.tile == 64 && n32 <= 2 * kUnits) {
             P.tm = (int)t32, P.tn = P.sym ? (int)t32 : (int)(p.lp / 32), P.tiles = (int)(n32 / count);
             const dim3 g((unsigned)n32);
-            // (no more loads a lane than its share of the sum has: with four times 16 k for all, a 256 x 256
-            // matrix takes 142 us)
+            // (no more loads a lane than its share of the sum has: 64 k for all cost 45% of a 256 x 256
+            // matrix' time)
             auto direct = [&](auto u) {
                 constexpr int U = decltype(u)::value;
                 return last ? launch(ortho_product32_kernel<U, true, T>, g, dim3(1024), s, P, M)
@@ -794,8 +797,8 @@ int run_large(const Mats& M, const OrthoPlan& p, int count, int steps, float ca,
         if (p.tile == 128) {
             // The last few tiles past a multiple of the compute units would be a round that few of them
             // share: their quarters go to as many, in a launch of their own.  Five steps with / without:
-            // 4096 x 4096 (528 tiles) 4767 / 5194 us, 3000 x 3000 (300) 2371 / 2585 us.  With up to 128 tiles
-            // so, 3400 x 3400 (378) would go from 3012 to 3175 us.
+            // 4096 x 4096 (528 tiles) 4240 / 4635 us, 3000 x 3000 (300) 2055 / 2295 us.  With up to 112 tiles
+            // so, 3300 x 3300 (351) would go from 2560 to 2640 us.
             const unsigned rest = g.x > 256 && g.x % 256 <= kTail ? g.x % 256 : 0;
             g.x -= rest;
             const int r = last ? launch(ortho_product_kernel<128, 1, 2, true, T>, g, dim3(256), s, P, M)
@@ -806,12 +809,14 @@ int run_large(const Mats& M, const OrthoPlan& p, int count, int steps, float ca,
         }
         // Up to one workgroup for every compute unit: four times the wavefronts share the sum's length, as
         // a single wavefront a SIMD waits for its own reads and products in turn.  Five steps with / without:
-        // one 1024 x 1024 matrix 229 / 242 us; with it up to 512 workgroups too, two of them 427 and not 347.
+        // one 1024 x 1024 matrix 215 / 302 us, 768 x 768 183 / 245; with it up to 400 workgroups too, 1536 x 1536 goes
+        // from 478 to 524.
         if (g.x <= kUnits)
             return last ? launch(ortho_product_kernel<64, 4, 2, true, T>, g, dim3(1024), s, P, M)
                         : launch(ortho_product_kernel<64, 4, 2, false, float>, g, dim3(1024), s, P, M);
-        return last ? launch(ortho_product_kernel<64, 1, 2, true, T>, g, dim3(256), s, P, M)
-                    : launch(ortho_product_kernel<64, 1, 2, false, float>, g, dim3(256), s, P, M);
+        // (three operand tiles, 48 KB, leave three workgroups a compute unit: 1536 x 1536 461 and not 480 us)
+        return last ? launch(ortho_product_kernel<64, 1, 3, true, T>, g, dim3(256), s, P, M)
+                    : launch(ortho_product_kernel<64, 1, 3, false, float>, g, dim3(256), s, P, M);
     };
     const Half none{nullptr, nullptr, 0, 0};
     for (int i = 0; i < steps && r == FPDE_OK; ++i) {
