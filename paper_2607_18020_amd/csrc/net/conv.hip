@@ -4,18 +4,19 @@
 //   dp = dy (silu'(p) = q (1 + p (1 - q)), q = sigmoid(p));  dx_t = sum_k w_k dp_{t + W - 1 - k}
 //   dw_k = sum_t dp_t x_{t - W + 1 + k},  db = sum_t dp_t
 //
-// A lane owns 4 neighbouring channels and marches a chunk of levels, the last W - 1 of
+// A lane owns 2 neighbouring channels and marches a chunk of levels, the last W - 1 of
 // them in registers, so x is read once but for the W - 1 levels before a chunk; the
 // next kBlock levels are on their way while those before them are worked on.  What
-// bounds both directions is memory: 4 channels (8 bytes of 16-bit data) a lane, not the
-// 8 of a 16-byte load, since the filters, windows and sums of 8 leave the backward one
-// wavefront a SIMD.  Where the channels are no multiple of 4 the last lane's four
-// begin earlier, and what two lanes own they write with the same values.  The backward
-// recomputes p from x instead of reading it, and runs W - 1 levels past its chunk for
-// the dp that dx needs there.
+// bounds both directions is memory, and how many loads are in flight: 2 channels (a
+// wavefront's load of 16-bit data is 256 bytes), since the filters, windows and sums of
+// 4 leave the backward two wavefronts a SIMD, of 8 one.  Where the channels are no
+// multiple of 2 the last lane's two begin earlier, and what two lanes own they write with
+// the same values.  The backward recomputes p from x instead of reading it, and runs
+// W - 1 levels past its chunk for the dp that dx needs there.
 //
-// Measured, 256 x 128 x 512 bf16, 4 taps: forward 17 us (4.0 TB/s), backward 34 and 5 for
-// the partial sums (3.0 TB/s); with 8 channels a lane both together 151 and not 57 us.
+// Measured, 256 x 128 x 512 bf16, 4 taps, with 2, 4 and 8 channels a lane: forward 15.6 us
+// (4.3 TB/s), 17.6, -, backward with 5 for the partial sums 30.8, 35.2, 130; 8 x 2048 x
+// 1024: 14.6 and 17.2, 28.1 and 33.8.
 #include "net_common.hpp"
 
 using namespace fpde_net;
@@ -23,6 +24,7 @@ using namespace fpde_net;
 namespace {
 
 constexpr int kBlock = 8;  // levels whose loads are in flight together
+constexpr int kLane = 2;   // channels of a lane
 
 struct ConvP {
     const void *x, *dy, *w, *b, *state;
@@ -140,7 +142,7 @@ __global__ __launch_bounds__(64) void conv_fwd_kernel(ConvP P) {
 }
 
 template <class T, int W, int V>
-__global__ __launch_bounds__(64) void conv_bwd_kernel(ConvP P) {
+__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(3))) void conv_bwd_kernel(ConvP P) {
     const int c = lane_channel<V>(P);
     if (c < 0) return;
     float w[W][V], bias[V], dw[W][V], db[V];
@@ -176,14 +178,14 @@ __global__ __launch_bounds__(64) void conv_bwd_kernel(ConvP P) {
                 load_block<T, V>(nx, P.x, b, P.xb, P.xt, t + kBlock, len, c);
                 load_block<T, V>(ng, P.dy, b, P.dyb, P.dyt, t + kBlock, len, c);
             }
-#pragma unroll
-            for (int j = 0; j < kBlock; ++j) {
-                if (t + j >= tn) break;
-                const bool own = t + j < t1;  // (the levels past the chunk count in the next one's dw)
+            // WHOLE: a level of the chunk that exists.  A block of them runs without a branch but that of the
+            // chunk's first stores, so the windows' shifts are names of registers and no moves.
+            auto level = [&](auto whole, int j) {
+                constexpr bool WHOLE = decltype(whole)::value;
                 float d[V], o[V];
 #pragma unroll
                 for (int i = 0; i < V; ++i) d[i] = 0.f;
-                if (t + j < len) {
+                if (WHOLE || t + j < len) {
                     float v[V];
                     unpack<T, V>(v, x[j]);
                     unpack<T, V>(d, g[j]);
@@ -201,7 +203,8 @@ __global__ __launch_bounds__(64) void conv_bwd_kernel(ConvP P) {
                             const float q = sigmoid(p);
                             d[i] *= q * fmaf(p, 1.f - q, 1.f);
                         }
-                        if (own) {
+                        // (the levels past the chunk count in the next one's dw)
+                        if (WHOLE || t + j < t1) {
                             db[i] += d[i];
 #pragma unroll
                             for (int k = 0; k < W; ++k) dw[k][i] = fmaf(d[i], win[k][i], dw[k][i]);
@@ -219,12 +222,22 @@ __global__ __launch_bounds__(64) void conv_bwd_kernel(ConvP P) {
                     for (int k = 0; k < W; ++k) o[i] = fmaf(w[k][i], dps[W - 1 - k][i], o[i]);
                 }
                 const int s = t + j - (W - 1);
-                if (s >= t0) {
-                    if (s >= len) {
+                if ((WHOLE && j >= W - 1) || s >= t0) {
+                    if (!WHOLE && s >= len) {
 #pragma unroll
                         for (int i = 0; i < V; ++i) o[i] = 0.f;
                     }
                     store_f32<T, V>(dx + (int64_t)s * P.channels, o, V);
+                }
+            };
+            if (t + kBlock <= t1 && t + kBlock <= len) {
+#pragma unroll
+                for (int j = 0; j < kBlock; ++j) level(std::true_type{}, j);
+            } else {
+#pragma unroll
+                for (int j = 0; j < kBlock; ++j) {
+                    if (t + j >= tn) break;
+                    level(std::false_type{}, j);
                 }
             }
 #pragma unroll
@@ -247,15 +260,15 @@ __global__ __launch_bounds__(64) void conv_bwd_kernel(ConvP P) {
 
 constexpr int64_t kMaxChannels = 1 << 20, kMaxLevels = (int64_t)1 << 34;
 // Wavefronts of a launch before they loop over chunks.  The backward's partial
-// sums grow with them (2048, 4096 and 8192 within 2% of each other at 256 x 128 x 512).
-constexpr int64_t kFwdWaves = 1 << 20, kBwdWaves = 4096;
+// sums grow with them (half and twice as many within 2% of these at 256 x 128 x 512).
+constexpr int64_t kFwdWaves = 1 << 21, kBwdWaves = 8192;
 
 // Levels of a chunk: 32, where the W - 1 levels read twice cost little, or 16 or 8 where
-// there would be fewer than one wavefront a SIMD.  Backward: 1 x 1024 x 512 19 us with 8 and 23 with 32; with
-// 64 throughout 8 x 2048 x 1024 takes 47 and not 38 us.
+// there would be fewer than one wavefront a SIMD.  Backward: 1 x 1024 x 512 19 us with 8 and 23 with 32;
+// 8 x 2048 x 1024 28 with 32, 34 with 16, 30 with 64.
 int chunk_of(int64_t batch, int64_t length, int64_t channels) {
     int c = 32;
-    while (c > 8 && batch * cdiv(length, c) * cdiv(channels, 256) < 1024) c /= 2;
+    while (c > 8 && batch * cdiv(length, c) * cdiv(channels, 64 * kLane) < 1024) c /= 2;
     return c;
 }
 
@@ -278,18 +291,18 @@ bool strides_ok(int64_t bs, int64_t ts, int64_t batch, int64_t length, int64_t c
 }
 
 int64_t slots(int64_t jobs, int64_t channels, int64_t waves) {
-    const int64_t n = waves / cdiv(channels, 256);
+    const int64_t n = waves / cdiv(channels, 64 * kLane);
     const int64_t m = n < 1 ? 1 : (n > 65535 ? 65535 : n);
     return jobs < m ? (jobs < 1 ? 1 : jobs) : m;
 }
 
-// f(T{}, integral_constant<int, taps>, integral_constant<int, channels a lane>): 4, or 1 where there
-// are fewer, or where lanes that share channels would read a state that the other replaces
+// f(T{}, integral_constant<int, taps>, integral_constant<int, channels a lane>): 2, or 1 where there
+// is one, or where lanes that share channels would read a state that the other replaces
 template <class F>
 int with_taps(int dtype, int taps, bool one, F f) {
     return with_type(dtype, [&](auto t) {
         auto v = [&](auto w) {
-            return one ? f(t, w, std::integral_constant<int, 1>{}) : f(t, w, std::integral_constant<int, 4>{});
+            return one ? f(t, w, std::integral_constant<int, 1>{}) : f(t, w, std::integral_constant<int, kLane>{});
         };
         switch (taps) {
         case 2: return v(std::integral_constant<int, 2>{});
@@ -329,7 +342,7 @@ extern "C" int fpde_causal_conv(const fpde_conv_args* a, void* stream) {
     P.wf32 = a->weight_dtype == FPDE_F32, P.silu = a->silu;
     P.chunk = chunk_of(a->batch, a->length, a->channels);
     P.chunks = a->length > 0 ? cdiv(a->length, P.chunk) : 1;
-    const bool one = a->channels < 4 || (a->channels % 4 && a->state && a->state == a->state_out);
+    const bool one = a->channels < kLane || (a->channels % kLane && a->state && a->state == a->state_out);
     return with_taps(a->dtype, a->taps, one, [&](auto t, auto w, auto v) {
         constexpr int V = decltype(v)::value;
         const dim3 g((unsigned)cdiv(a->channels, 64 * V),
@@ -384,7 +397,7 @@ extern "C" int fpde_causal_conv_bwd(const fpde_conv_bwd_args* a, void* stream) {
     P.part = (float*)a->workspace;
     hipStream_t s = (hipStream_t)stream;
     if (jobs > 0) {
-        st = with_taps(a->dtype, a->taps, a->channels < 4, [&](auto t, auto w, auto v) {
+        st = with_taps(a->dtype, a->taps, a->channels < kLane, [&](auto t, auto w, auto v) {
             constexpr int V = decltype(v)::value;
             return launch(conv_bwd_kernel<decltype(t), decltype(w)::value, V>,
                           dim3((unsigned)cdiv(a->channels, 64 * V), (unsigned)n), dim3(64), s, P);
