@@ -799,7 +799,7 @@ int run_large(const Mats& M, const OrthoPlan& p, int count, int steps, float ca,
             // share: their quarters go to as many, in a launch of their own.  Five steps with / without:
             // 4096 x 4096 (528 tiles) 4240 / 4635 us, 3000 x 3000 (300) 2055 / 2295 us.  With up to 112 tiles
             // so, 3300 x 3300 (351) would go from 2560 to 2640 us.
-            const unsigned rest = g.x > 256 && g.x % 256 <= kTail ? g.x % 256 : 0;
+            const unsigned rest = g.x > kUnits && g.x % kUnits <= kTail ? g.x % kUnits : 0;
             g.x -= rest;
             const int r = last ? launch(ortho_product_kernel<128, 1, 2, true, T>, g, dim3(256), s, P, M)
                                : launch(ortho_product_kernel<128, 1, 2, false, float>, g, dim3(256), s, P, M);
