@@ -16,7 +16,8 @@ answers one level at a time; its fields go into ``binding.ResidualLoss`` or
 
 The functions with a C name queue the library's kernels on the current stream
 (or ``stream``) and return tensors; the classes wrap them for autograd and
-optimisers.  As in ``binding``, this module marshals arguments only: there is no
+optimisers.  Tensors that a call writes in place count as changed for autograd.  As
+in ``binding``, this module marshals arguments only: there is no
 fallback, and importing a call without the built library fails loudly.  Data
 tensors are float32, bfloat16 or float16 CUDA tensors on the current device.
 """
@@ -29,6 +30,7 @@ from typing import Optional
 
 import torch
 from torch.autograd.function import once_differentiable
+from torch.autograd.graph import increment_version
 
 from .binding import FPDE_OK, FpdeError, _raw_stream, _stream
 
@@ -226,6 +228,11 @@ def _levels(what, name, t):
     return (*t.shape, t.stride(0), t.stride(1))
 
 
+# A tensor of the caller's that a call writes gets the next version, as in torch's own in-place
+# operations: a backward pass that has saved it then raises instead of using what was written over it.
+_written = increment_version
+
+
 def _empty(stream, shape, dtype, dev):
     if stream is None:
         return torch.empty(shape, dtype=dtype, device=dev)
@@ -260,6 +267,7 @@ def fpde_rms_norm(x, weight=None, *, residual=None, eps: float = 1e-6, quant: Op
     code = _data("fpde_rms_norm", "x", x)
     dev, dt = x.device, x.dtype
     rows, width, xs = _rows("fpde_rms_norm", "x", x)
+    given = [t for t in (out, sum_out) if t is not None]
     rp = rs = sp = None
     if residual is not None:
         rp = _like("fpde_rms_norm", "residual", residual, x)
@@ -284,6 +292,8 @@ def fpde_rms_norm(x, weight=None, *, residual=None, eps: float = 1e-6, quant: Op
     a = NormArgs(code, wcode, code if quant is None else _F8, quant or 0, rows, width, xs, rs or 0, eps,
                  x.data_ptr(), rp, wp, out.data_ptr(), sp, None if scales is None else scales.data_ptr())
     _call("fpde_rms_norm", a, stream)
+    if given:
+        _written(given)
     s = x if sum_out is None else sum_out
     return (out, s) if quant is None else (out, scales, s)
 
@@ -308,14 +318,18 @@ def fpde_rms_norm_bwd(dy, s, weight=None, *, dsum=None, eps: float = 1e-6, want_
         wp, wcode = _param("fpde_rms_norm_bwd", "weight", weight, (width,), dt, dev), _CODES[weight.dtype]
         if want_dweight:
             dweight = _empty(stream, (width,), weight.dtype, dev)
+    given = False
     if ds is None:
         ds = _empty_like(stream, dy)
     else:
         _dense("fpde_rms_norm_bwd", "ds", ds, dy.shape, dt, dev)
+        given = True
     a = NormBwdArgs(code, wcode, rows, width, dys, ss, dss, eps, dy.data_ptr(), s.data_ptr(), dp, wp,
                     ds.data_ptr(), None if dweight is None else dweight.data_ptr(), None, 0)
     _workspace("fpde_rms_norm_bwd", a, dev, stream)
     _call("fpde_rms_norm_bwd", a, stream)
+    if given:
+        _written(ds)
     return ds, dweight
 
 
@@ -368,12 +382,15 @@ def fpde_causal_conv(x, weight, bias=None, *, silu: bool = True, state=None, len
     code, B, L, D, bs, ts, W, wp, bp, sp, lp = _conv_common(what, x, weight, bias, state, lengths)
     dev, dt = x.device, x.dtype
     so = None if state_out is None else _dense(what, "state_out", state_out, (B, W - 1, D), dt, dev)
+    given = [t for t in (out, state_out) if t is not None]
     if out is None:
         out = _empty(stream, (B, L, D), dt, dev)
     else:
         _dense(what, "out", out, (B, L, D), dt, dev)
     _call(what, ConvArgs(code, _CODES[weight.dtype], W, bool(silu), B, L, D, bs, ts, x.data_ptr(), wp, bp, sp, lp,
                          out.data_ptr(), so), stream)
+    if given:
+        _written(given)
     return out
 
 
@@ -387,6 +404,7 @@ def fpde_causal_conv_step(x, state, weight, bias=None, *, silu: bool = True, out
     dev, dt = x.device, x.dtype
     B, D = x.shape
     W = weight.shape[1]
+    given = state if out is None else (state, out)
     if out is None:
         out = _empty_like(stream, x)
     else:
@@ -396,6 +414,7 @@ def fpde_causal_conv_step(x, state, weight, bias=None, *, silu: bool = True, out
     sp = _dense(what, "state", state, (B, W - 1, D), dt, dev)
     _call("fpde_causal_conv", ConvArgs(code, _CODES[weight.dtype], W, bool(silu), B, 1, D, x.stride(0), D,
                                        x.data_ptr(), wp, bp, sp, None, out.data_ptr(), sp), stream)
+    _written(given)
     return out
 
 
@@ -489,6 +508,7 @@ def fpde_selective_scan(u, delta, A, B, C, *, D=None, z=None, delta_bias=None, s
     head, ptrs, (Bn, L, Dn, _, n) = _scan_common(what, u, delta, A, B, C, D, z, delta_bias, softplus, state, lengths)
     dev, dt = u.device, u.dtype
     so = None if state_out is None else _dense(what, "state_out", state_out, (Bn, Dn, n), torch.float32, dev)
+    given = [t for t in (out, state_out) if t is not None]
     if out is None:
         out = _empty(stream, (Bn, L, Dn), dt, dev)
     else:
@@ -497,6 +517,8 @@ def fpde_selective_scan(u, delta, A, B, C, *, D=None, z=None, delta_bias=None, s
     if L > 1:
         _workspace(what, a, dev, stream)
     _call(what, a, stream)
+    if given:
+        _written(given)
     return out
 
 
@@ -530,6 +552,7 @@ def fpde_selective_step(state, u, delta, A, B, C, *, D=None, z=None, delta_bias=
         if (n > 1 and t.stride(-1) != 1) or (groups > 1 and t.stride(1) != n):
             raise ValueError(f"{what} {name}: groups and states have to be dense")
         strides += (t.stride(0), groups * n)
+    given = state if out is None else (state, out)
     if out is None:
         out = _empty_like(stream, u)
     else:
@@ -541,6 +564,7 @@ def fpde_selective_step(state, u, delta, A, B, C, *, D=None, z=None, delta_bias=
         None if D is None else _dense(what, "D", D, (Dn,), f32, dev), None if z is None else z.data_ptr(),
         None if delta_bias is None else _dense(what, "delta_bias", delta_bias, (Dn,), f32, dev), sp, None,
         out.data_ptr(), sp, None, 0), stream)
+    _written(given)
     return out
 
 
@@ -615,7 +639,7 @@ def fpde_orthogonalize(mats, *, steps: int = 5, coeffs=NS_COEFFS, eps: float = 1
     [..., m, n] tensor, or a sequence of dense [m, n] tensors of one shape; returns the
     same (``out``: where to, like ``mats``, or ``mats`` itself)."""
     what = "fpde_orthogonalize"
-    one = isinstance(mats, torch.Tensor)
+    one, given = isinstance(mats, torch.Tensor), out is not None
     if one:
         code = _data(what, "input", mats)
         if mats.dim() < 2 or not mats.is_contiguous():
@@ -646,6 +670,8 @@ def fpde_orthogonalize(mats, *, steps: int = 5, coeffs=NS_COEFFS, eps: float = 1
     a = OrthoArgs(code, steps, count, m, n, *coeffs, eps, ctypes.cast(gp, _vp), ctypes.cast(op, _vp), None, 0)
     _workspace(what, a, dev, stream)
     _call(what, a, stream)
+    if given:
+        _written(out)
     return out
 
 
@@ -678,6 +704,7 @@ def fpde_muon_step(weights, grads, momenta, *, lr: float, momentum: float = 0.95
                  ctypes.cast(gp, _vp), ctypes.cast(mp, _vp), ctypes.cast(wp, _vp), None, 0)
     _workspace(what, a, weights[0].device, stream)
     _call(what, a, stream)
+    _written(weights + momenta)
 
 
 class Muon(torch.optim.Optimizer):
