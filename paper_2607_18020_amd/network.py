@@ -180,14 +180,14 @@ def _data(what, name, t):
 
 def _like(what, name, t, x):
     """A tensor of x's shape, type and device; its strides are its own."""
-    if not isinstance(t, _Tensor) or t.shape != x.shape or t.dtype is not x.dtype or t.device != x.device:
+    if not isinstance(t, _Tensor) or t.shape != x.shape or t.dtype is not x.dtype or t.get_device() != x.get_device():
         raise ValueError(f"{what} {name}: need a tensor like the first, {tuple(x.shape)} {x.dtype} on {x.device}")
     return t.data_ptr()
 
 
 def _dense(what, name, t, shape, dtype, dev):
     """A dense tensor of this shape, type and device."""
-    if not isinstance(t, _Tensor) or t.dtype is not dtype or t.shape != shape or t.device != dev \
+    if not isinstance(t, _Tensor) or t.dtype is not dtype or t.shape != shape or t.get_device() != dev.index \
             or not t.is_contiguous():
         raise ValueError(f"{what} {name}: need a contiguous {dtype} tensor of shape {tuple(shape)} on {dev}")
     return t.data_ptr()
@@ -223,9 +223,13 @@ def _rows(what, name, t):
 
 def _levels(what, name, t):
     """(batch, length, channels, batch stride, time stride) of a [B, L, D] tensor."""
-    if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
-        raise ValueError(f"{what} {name}: need [batch, length, channels] with dense channels")
-    return (*t.shape, t.stride(0), t.stride(1))
+    if t.dim() == 3:
+        B, L, D = t.shape
+        if t.is_contiguous():
+            return B, L, D, L * D, D
+        if D <= 1 or t.stride(2) == 1:
+            return B, L, D, t.stride(0), t.stride(1)
+    raise ValueError(f"{what} {name}: need [batch, length, channels] with dense channels")
 
 
 # A tensor of the caller's that a call writes gets the next version, as in torch's own in-place
@@ -267,11 +271,11 @@ def fpde_rms_norm(x, weight=None, *, residual=None, eps: float = 1e-6, quant: Op
     code = _data("fpde_rms_norm", "x", x)
     dev, dt = x.device, x.dtype
     rows, width, xs = _rows("fpde_rms_norm", "x", x)
-    given = [t for t in (out, sum_out) if t is not None]
+    given = None if out is None and sum_out is None else [t for t in (out, sum_out) if t is not None]
     rp = rs = sp = None
     if residual is not None:
         rp = _like("fpde_rms_norm", "residual", residual, x)
-        rs = _rows("fpde_rms_norm", "residual", residual)[2]
+        rs = width if residual.is_contiguous() else _rows("fpde_rms_norm", "residual", residual)[2]
     if sum_out is not None:
         sp = _dense("fpde_rms_norm", "sum_out", sum_out, x.shape, dt, dev)
     elif residual is not None:
@@ -382,9 +386,9 @@ def fpde_causal_conv(x, weight, bias=None, *, silu: bool = True, state=None, len
     code, B, L, D, bs, ts, W, wp, bp, sp, lp = _conv_common(what, x, weight, bias, state, lengths)
     dev, dt = x.device, x.dtype
     so = None if state_out is None else _dense(what, "state_out", state_out, (B, W - 1, D), dt, dev)
-    given = [t for t in (out, state_out) if t is not None]
+    given = None if out is None and state_out is None else [t for t in (out, state_out) if t is not None]
     if out is None:
-        out = _empty(stream, (B, L, D), dt, dev)
+        out = _empty_like(stream, x)
     else:
         _dense(what, "out", out, (B, L, D), dt, dev)
     _call(what, ConvArgs(code, _CODES[weight.dtype], W, bool(silu), B, L, D, bs, ts, x.data_ptr(), wp, bp, sp, lp,
@@ -399,7 +403,9 @@ def fpde_causal_conv_step(x, state, weight, bias=None, *, silu: bool = True, out
     and updated in place.  Returns y [B, D]."""
     what = "fpde_causal_conv_step"
     code = _data(what, "x", x)
-    if x.dim() != 2 or not isinstance(weight, _Tensor) or weight.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
+    dense = x.is_contiguous()
+    if x.dim() != 2 or not isinstance(weight, _Tensor) or weight.dim() != 2 \
+            or not (dense or x.shape[1] <= 1 or x.stride(1) == 1):
         raise ValueError(f"{what}: need x [batch, channels] with dense channels and weight [channels, taps]")
     dev, dt = x.device, x.dtype
     B, D = x.shape
@@ -412,7 +418,7 @@ def fpde_causal_conv_step(x, state, weight, bias=None, *, silu: bool = True, out
     wp = _param(what, "weight", weight, (D, W), dt, dev)
     bp = None if bias is None else _dense(what, "bias", bias, (D,), weight.dtype, dev)
     sp = _dense(what, "state", state, (B, W - 1, D), dt, dev)
-    _call("fpde_causal_conv", ConvArgs(code, _CODES[weight.dtype], W, bool(silu), B, 1, D, x.stride(0), D,
+    _call("fpde_causal_conv", ConvArgs(code, _CODES[weight.dtype], W, bool(silu), B, 1, D, D if dense else x.stride(0), D,
                                        x.data_ptr(), wp, bp, sp, None, out.data_ptr(), sp), stream)
     _written(given)
     return out
@@ -477,7 +483,7 @@ def _scan_common(what, u, delta, A, B, C, D, z, delta_bias, softplus, state, len
         strides += _levels(what, name, t)[3:]
     groups = B.shape[2] if isinstance(B, torch.Tensor) and B.dim() == 4 else 1
     for name, t in (("B", B), ("C", C)):
-        if not isinstance(t, _Tensor) or t.dtype is not dt or t.device != dev:
+        if not isinstance(t, _Tensor) or t.dtype is not dt or t.get_device() != dev.index:
             raise ValueError(f"{what} {name}: need a {dt} tensor on {dev}")
         if t.shape != (Bn, L, groups, n) and (groups > 1 or t.shape != (Bn, L, n)):
             raise ValueError(f"{what} {name}: need [batch, length, groups, states] (or without groups)")
@@ -508,9 +514,9 @@ def fpde_selective_scan(u, delta, A, B, C, *, D=None, z=None, delta_bias=None, s
     head, ptrs, (Bn, L, Dn, _, n) = _scan_common(what, u, delta, A, B, C, D, z, delta_bias, softplus, state, lengths)
     dev, dt = u.device, u.dtype
     so = None if state_out is None else _dense(what, "state_out", state_out, (Bn, Dn, n), torch.float32, dev)
-    given = [t for t in (out, state_out) if t is not None]
+    given = None if out is None and state_out is None else [t for t in (out, state_out) if t is not None]
     if out is None:
-        out = _empty(stream, (Bn, L, Dn), dt, dev)
+        out = _empty_like(stream, u)
     else:
         _dense(what, "out", out, (Bn, L, Dn), dt, dev)
     a = ScanArgs(*head, *ptrs, out.data_ptr(), so, None, 0)
@@ -540,18 +546,26 @@ def fpde_selective_step(state, u, delta, A, B, C, *, D=None, z=None, delta_bias=
         if t is None and name == "z":
             strides += (0, 0)
             continue
-        _like(what, name, t, u)
-        if Dn > 1 and t.stride(1) != 1:
+        if t is not u:
+            _like(what, name, t, u)
+        if t.is_contiguous():
+            strides += (Dn, Dn)
+        elif Dn > 1 and t.stride(1) != 1:
             raise ValueError(f"{what} {name}: channels have to be dense")
-        strides += (t.stride(0), Dn)
+        else:
+            strides += (t.stride(0), Dn)
+    index, bc = dev.index, groups * n
     for name, t in (("B", B), ("C", C)):
-        if not isinstance(t, _Tensor) or t.dtype is not dt or t.device != dev:
+        if not isinstance(t, _Tensor) or t.dtype is not dt or t.get_device() != index:
             raise ValueError(f"{what} {name}: need a {dt} tensor on {dev}")
         if t.shape != (Bn, groups, n) and (groups > 1 or t.shape != (Bn, n)):
             raise ValueError(f"{what} {name}: need [batch, groups, states] (or without groups)")
-        if (n > 1 and t.stride(-1) != 1) or (groups > 1 and t.stride(1) != n):
+        if t.is_contiguous():
+            strides += (bc, bc)
+        elif (n > 1 and t.stride(-1) != 1) or (groups > 1 and t.stride(1) != n):
             raise ValueError(f"{what} {name}: groups and states have to be dense")
-        strides += (t.stride(0), groups * n)
+        else:
+            strides += (t.stride(0), bc)
     given = state if out is None else (state, out)
     if out is None:
         out = _empty_like(stream, u)
